@@ -486,6 +486,98 @@ enum {
 };
 int mfsgd_debug_read(int32_t what, void* dst, int64_t count, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators on tables of rows (the trained factors, or any caller-owned table
+ * like them).  They act on caller-owned device memory of the current device,
+ * need no mfsgd_init unless they say so, use nothing of the context but the
+ * error text, only enqueue kernels (no allocation, copy, memset or wait: they
+ * may be captured into a HIP graph) and give the same bits every time.  Two of
+ * them may run at once on different streams with workspaces of their own.
+ *   - `dtype` is MFSGD_FP32, MFSGD_FP16 or MFSGD_BF16 (the operators alone:
+ *     bfloat16); all arrays of a call have it.  Arithmetic and sums are
+ *     binary32, each result is rounded once, to nearest even.
+ *   - Matrices are row-major; `ld...` is the distance between rows in elements,
+ *     at least the row's width.  A pointer needs the alignment of one element.
+ *     Arrays must not overlap unless a call says they may.
+ *   - A workspace is device memory of at least the bytes that the matching
+ *     ..._workspace call gives (0: none needed, NULL is fine), aligned to 256
+ *     bytes; its content before and after is of no meaning.  It must not be
+ *     used by anything else until the work enqueued on it has completed.
+ *   - MFSGD_EINVAL for a negative size, a NULL array that has elements, an ld
+ *     below the width, an unknown dtype, a pointer not aligned to its element
+ *     and a workspace that is too small or misaligned; MFSGD_EHIP for a launch
+ *     failure.  Nothing is enqueued on MFSGD_EINVAL. */
+enum { MFSGD_BF16 = 2 };
+
+/* Rows by id: out[i, 0..k) = scale * table[ids[i], 0..k) for i in [0, count).
+ * ids[i] is read at ids + i * ids_stride, so a column of an mfsgd_sample array
+ * (stride 3) is an id array.  An id outside [0, rows) stands for no row
+ * (padding): its row of `out` is zero.  rows in [1, 2^31-1], k and ids_stride
+ * at least 1, count at most 2^31-1. */
+int mfsgd_embed(const void* table, int64_t rows, int64_t ld, int32_t k, int32_t dtype, const int32_t* ids,
+                int64_t ids_stride, int64_t count, float scale, void* out, int64_t ld_out, void* stream);
+
+/* Its gradient with respect to the table, for dout with the shape of `out`:
+ *   dtable[r, :] = (accumulate ? dtable[r, :] : 0)
+ *                  + scale * sum over the i with ids[i] = r of dout[i, :]
+ * for every r in [0, rows); tokens whose id stands for no row are left out.
+ * With `accumulate` only the rows of `ids` are read and written: with scale =
+ * -lr this is the gradient step of those rows, in place.  A row's tokens are
+ * added in a fixed order (no atomics on values). */
+int mfsgd_embed_grad(const void* dout, int64_t ld_dout, const int32_t* ids, int64_t ids_stride, int64_t count,
+                     int32_t k, int32_t dtype, float scale, void* dtable, int64_t rows, int64_t ld,
+                     int32_t accumulate, void* workspace, int64_t workspace_bytes, void* stream);
+int mfsgd_embed_grad_workspace(int64_t count, int32_t k, int64_t* bytes);
+
+/* The two on the model's own factors (after mfsgd_init; the current device must
+ * be the one it ran on): `side` is MFSGD_P (users, m rows) or MFSGD_Q (items, n
+ * rows), k and dtype must be the model's.
+ * mfsgd_add_rows updates the factors in place as mfsgd_embed_grad does with
+ * `accumulate` (workspace: mfsgd_embed_grad_workspace).  Ordered on `stream`
+ * like an epoch.  ESTATE before mfsgd_init or on another device. */
+enum { MFSGD_P = 0, MFSGD_Q = 1 };
+int mfsgd_rows(int32_t side, const int32_t* ids, int64_t ids_stride, int64_t count, int32_t k, int32_t dtype,
+               float scale, void* out, int64_t ld_out, void* stream);
+int mfsgd_add_rows(int32_t side, const void* dout, int64_t ld_dout, const int32_t* ids, int64_t ids_stride,
+                   int64_t count, int32_t k, int32_t dtype, float scale, void* workspace, int64_t workspace_bytes,
+                   void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The global norm of many gradients, and clipping by it.  Conventions as for
+ * the operators above, except that every tensor has a dtype of its own; `list`
+ * is HOST memory, read before the call returns.
+ *   norm = sqrt(sum over all tensors and elements of g^2)   (binary64)
+ *   c    = norm <= max_norm ? 1 : max_norm / norm
+ * A gradient that is not finite makes norm infinite or NaN and c 0 or NaN, as
+ * the formula gives them (a NaN then reaches every element): the caller sees it
+ * in *norm_dev.
+ * Every call writes the norm to *norm_dev, one binary64 in caller-owned DEVICE
+ * memory (0 for no elements). */
+typedef struct {
+    void* data;    /* device memory, n contiguous elements */
+    int64_t n;
+    int32_t dtype;
+    int32_t unused; /* 0 */
+} mfsgd_tensor;
+
+/* The norm alone.  A tensor may appear more than once (it then counts so). */
+int mfsgd_grad_norm(const mfsgd_tensor* grads, int64_t count, double* norm_dev, void* workspace,
+                    int64_t workspace_bytes, void* stream);
+/* g <- c g in place.  EINVAL also for a max_norm that is negative or NaN and for
+ * tensors that overlap. */
+int mfsgd_clip_grads(const mfsgd_tensor* grads, int64_t count, double max_norm, double* norm_dev, void* workspace,
+                     int64_t workspace_bytes, void* stream);
+/* The clipped SGD update with the regularisation of section 2.2, in one pass:
+ *   p <- p - lr * (c g + lambda p)
+ * for params[i] and grads[i] of one n and dtype each; the gradients stay as they
+ * are.  max_norm may be infinite (no clipping).  EINVAL also for a non-finite lr
+ * or lambda, for params that overlap each other or any of grads, and for pairs
+ * that differ in n or dtype. */
+int mfsgd_sgd_step(const mfsgd_tensor* params, const mfsgd_tensor* grads, int64_t count, float lr, float lambda,
+                   double max_norm, double* norm_dev, void* workspace, int64_t workspace_bytes, void* stream);
+/* Workspace of the three for up to `count` tensors. */
+int mfsgd_norm_workspace(int64_t count, int64_t* bytes);
+
 /* Release everything; the context returns to the un-initialised state. */
 int mfsgd_finalize(void);
 

@@ -14,18 +14,24 @@ import subprocess
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
+CSRC_OPS = os.path.join(PKG, "csrc_ops")  # the operators: apart from the epochs' sources, which carry their profiles
 INCLUDE = os.path.join(ROOT, "include")
 OBJDIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmfsgd.so")
-SOURCES = ["mfsgd_api.hip", "mfsgd_aux.hip", "mfsgd_table.hip", "mfsgd_kernels_f32.hip", "mfsgd_kernels_f16.hip"]
+SOURCES = ["mfsgd_api.hip", "mfsgd_aux.hip", "mfsgd_table.hip", "mfsgd_kernels_f32.hip", "mfsgd_kernels_f16.hip",
+           "ops_api.hip", "ops_rows.hip", "ops_norm.hip"]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 CFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    "-I", INCLUDE, "-I", CSRC,
+    "-I", INCLUDE, "-I", CSRC, "-I", CSRC_OPS,
 ]
+
+
+def _path(src: str) -> str:
+    return os.path.join(CSRC_OPS if src.startswith("ops_") else CSRC, src)
 
 
 def _inputs_digest(src: str) -> str:
@@ -33,7 +39,9 @@ def _inputs_digest(src: str) -> str:
     beside it and the public headers (taken before compiling, so an edit made
     while the compiler runs leaves the object marked stale)."""
     h = hashlib.sha256()
-    deps = [os.path.join(CSRC, src)] + sorted(os.path.join(CSRC, x) for x in os.listdir(CSRC) if x.endswith(".hpp"))
+    deps = [_path(src)] + sorted(os.path.join(CSRC, x) for x in os.listdir(CSRC) if x.endswith(".hpp"))
+    if src.startswith("ops_"):
+        deps += sorted(os.path.join(CSRC_OPS, x) for x in os.listdir(CSRC_OPS) if x.endswith(".hpp"))
     deps += sorted(os.path.join(INCLUDE, x) for x in os.listdir(INCLUDE))
     for d in deps:
         with open(d, "rb") as f:
@@ -46,7 +54,7 @@ def _inputs_digest(src: str) -> str:
 def _compile(src: str) -> str:
     obj = os.path.join(OBJDIR, os.path.splitext(src)[0] + ".o")
     digest = _inputs_digest(src)
-    cmd = [HIPCC, *CFLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = [HIPCC, *CFLAGS, "-c", _path(src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed for {src}:\n{r.stderr}")

@@ -1857,6 +1857,26 @@ int debug_read_impl(int32_t what, void* dst, int64_t count, hipStream_t st)
 
 } // namespace
 
+namespace mfsgd {
+
+int set_error(int code, const char* msg) noexcept
+{
+    try {
+        g_err = msg;
+    } catch (...) {
+        g_err.clear();
+    }
+    return code;
+}
+
+bool model_view(ModelView* v) noexcept
+{
+    *v = ModelView{g.P, g.Q, g.m, g.n, g.k, g.KP, g.dtype, g.device};
+    return g.inited;
+}
+
+} // namespace mfsgd
+
 extern "C" {
 
 int mfsgd_set_option(const char* key, int64_t value)

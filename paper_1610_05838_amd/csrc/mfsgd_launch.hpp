@@ -99,6 +99,17 @@ struct TableLaunch {
     int32_t* trace;        // 3 per decision: block, claim stamp, release stamp
 };
 
+// What the operators (csrc_ops/) see of the API layer, implemented in
+// mfsgd_api.hip: the last error's text, and the model's factors in place.
+struct ModelView {
+    void* P;          // m rows of KP values, the first k of them the model's
+    void* Q;          // n rows
+    int64_t m, n;
+    int k, KP, dtype, device;
+};
+int set_error(int code, const char* msg) noexcept; // returns `code`
+bool model_view(ModelView* v) noexcept;            // false before mfsgd_init
+
 // Implemented per storage type in mfsgd_kernels_f32.hip / mfsgd_kernels_f16.hip.
 hipError_t epoch_f32(const EpochLaunch& a, hipStream_t st);
 hipError_t epoch_f16(const EpochLaunch& a, hipStream_t st);

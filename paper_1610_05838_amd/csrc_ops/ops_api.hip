@@ -1,0 +1,294 @@
+// ops_api.hip -- the C ABI of the operators (include/mfsgd.h): argument checks
+// and dispatch.  They keep no state; the model's factors and the error text
+// come from mfsgd_api.hip.
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+#include <new>
+#include <vector>
+
+#include "mfsgd.h"
+#include "mfsgd_launch.hpp"
+#include "ops_launch.hpp"
+
+namespace {
+
+using namespace mfsgd;
+using namespace mfsgd::ops;
+
+static_assert(kF32 == MFSGD_FP32 && kF16 == MFSGD_FP16 && kBF16 == MFSGD_BF16, "element types");
+
+int bad(const char* msg) { return set_error(MFSGD_EINVAL, msg); }
+
+int launched(hipError_t e) { return e == hipSuccess ? MFSGD_OK : set_error(MFSGD_EHIP, hipGetErrorString(e)); }
+
+// No exception crosses the ABI; a call that returns MFSGD_OK leaves no text.
+template <typename F>
+int guarded(F&& f) noexcept
+{
+    try {
+        set_error(MFSGD_OK, "");
+        return f();
+    } catch (const std::bad_alloc&) {
+        return set_error(MFSGD_ENOMEM, "host allocation failed");
+    } catch (...) {
+        return set_error(MFSGD_EHIP, "unexpected exception");
+    }
+}
+
+#define REQUIRE(cond, msg)                                                                                         \
+    do {                                                                                                           \
+        if (!(cond))                                                                                               \
+            return bad(msg);                                                                                       \
+    } while (0)
+
+bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+// rows x width elements at p, rows ld elements apart: present, aligned, and its extent in bytes fits 62 bits
+bool matrix_ok(const void* p, int64_t rows, int64_t width, int64_t ld, int dtype)
+{
+    if (ld < width || ld > (int64_t(1) << 40))
+        return false;
+    if (rows == 0 || width == 0)
+        return true;
+    return p && aligned(p, elem_bytes(dtype)) && (rows - 1 < (int64_t(1) << 60) / ((int64_t)elem_bytes(dtype) * ld));
+}
+
+bool dtype_ok(int32_t d) { return d == kF32 || d == kF16 || d == kBF16; }
+
+int check_work(const void* work, int64_t have, size_t need)
+{
+    REQUIRE(need == 0 || (work && have >= 0 && (uint64_t)have >= need), "the workspace is too small");
+    REQUIRE(need == 0 || aligned(work, 256), "the workspace is not aligned to 256 bytes");
+    return MFSGD_OK;
+}
+
+int check_ids(const int32_t* ids, int64_t stride, int64_t count)
+{
+    REQUIRE(count >= 0 && count <= INT32_MAX, "count must be in [0, 2^31-1]");
+    REQUIRE(stride >= 1 && stride <= (int64_t(1) << 28), "ids_stride must be in [1, 2^28]");
+    REQUIRE(count == 0 || (ids && aligned(ids, 4)), "ids is NULL or not aligned to 4 bytes");
+    return MFSGD_OK;
+}
+
+int embed_impl(const RowsLaunch& a, void* stream)
+{
+    REQUIRE(dtype_ok(a.dtype), "unknown dtype");
+    REQUIRE(a.rows >= 1 && a.rows <= INT32_MAX, "rows must be in [1, 2^31-1]");
+    REQUIRE(a.k >= 1, "k must be at least 1");
+    if (int rc = check_ids(a.ids, a.ids_stride, a.count))
+        return rc;
+    REQUIRE(matrix_ok(a.table, a.rows, a.k, a.ld, a.dtype), "table is NULL or misaligned, or ld is below k");
+    REQUIRE(matrix_ok(a.out, a.count, a.k, a.ld_out, a.dtype), "out is NULL or misaligned, or ld_out is below k");
+    return a.count ? launched(rows_get(a, (hipStream_t)stream)) : MFSGD_OK;
+}
+
+int embed_grad_impl(RowsGradLaunch a, void* work, int64_t bytes, void* stream)
+{
+    REQUIRE(dtype_ok(a.dtype), "unknown dtype");
+    REQUIRE(a.rows >= 1 && a.rows <= INT32_MAX, "rows must be in [1, 2^31-1]");
+    REQUIRE(a.k >= 1, "k must be at least 1");
+    if (int rc = check_ids(a.ids, a.ids_stride, a.count))
+        return rc;
+    REQUIRE(matrix_ok(a.dout, a.count, a.k, a.ld_dout, a.dtype), "dout is NULL or misaligned, or ld_dout is below k");
+    REQUIRE(matrix_ok(a.dtable, a.rows, a.k, a.ld, a.dtype), "dtable is NULL or misaligned, or ld is below k");
+    if (int rc = check_work(work, bytes, rows_grad_bytes(a.count, a.k)))
+        return rc;
+    a.work = work;
+    return launched(rows_grad(a, (hipStream_t)stream));
+}
+
+// The model's table of `side`, if the current device holds it.
+int table_of(int32_t side, int32_t k, int32_t dtype, ModelView& v, void*& table, int64_t& rows)
+{
+    int dev = -1;
+    if (!model_view(&v))
+        return set_error(MFSGD_ESTATE, "mfsgd_init has not been called");
+    if (hipGetDevice(&dev) != hipSuccess || dev != v.device)
+        return set_error(MFSGD_ESTATE, "the current device is not the one mfsgd_init ran on");
+    REQUIRE(side == MFSGD_P || side == MFSGD_Q, "side must be MFSGD_P or MFSGD_Q");
+    REQUIRE(k == v.k && dtype == v.dtype, "k or dtype is not the model's");
+    table = side == MFSGD_P ? v.P : v.Q;
+    rows = side == MFSGD_P ? v.m : v.n;
+    return MFSGD_OK;
+}
+
+// ---- norms ----
+
+constexpr int64_t kMostTensors = 1 << 20;
+
+int check_tensors(const mfsgd_tensor* list, int64_t count)
+{
+    REQUIRE(count >= 0 && count <= kMostTensors, "the number of tensors must be in [0, 2^20]");
+    REQUIRE(count == 0 || list, "NULL list of tensors");
+    int64_t all = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        const mfsgd_tensor& t = list[i];
+        REQUIRE(dtype_ok(t.dtype), "unknown dtype");
+        REQUIRE(t.n >= 0 && t.n <= (int64_t(1) << 40), "a tensor's n must be in [0, 2^40]");
+        REQUIRE(t.n == 0 || (t.data && aligned(t.data, elem_bytes(t.dtype))), "a tensor is NULL or misaligned");
+        all += t.n;
+        REQUIRE(all <= (int64_t(1) << 43), "the tensors hold more than 2^43 elements");
+    }
+    return MFSGD_OK;
+}
+
+struct Span {
+    uintptr_t from, to;
+    bool written;
+};
+
+void add_spans(std::vector<Span>& s, const mfsgd_tensor* list, int64_t count, bool written)
+{
+    for (int64_t i = 0; i < count; ++i)
+        if (list[i].n)
+            s.push_back(Span{(uintptr_t)list[i].data,
+                             (uintptr_t)list[i].data + (size_t)list[i].n * elem_bytes(list[i].dtype), written});
+}
+
+// Whether a written span shares a byte with any other.
+bool overlap(std::vector<Span>& s)
+{
+    std::sort(s.begin(), s.end(), [](const Span& a, const Span& b) { return a.from < b.from; });
+    uintptr_t any = 0, written = 0; // furthest ends so far
+    for (const Span& x : s) {
+        if (x.from < written || (x.written && x.from < any))
+            return true;
+        any = std::max(any, x.to);
+        if (x.written)
+            written = std::max(written, x.to);
+    }
+    return false;
+}
+
+int norm_impl(const mfsgd_tensor* params, const mfsgd_tensor* grads, int64_t count, int apply, float lr, float lam,
+              double max_norm, double* norm_dev, void* work, int64_t bytes, void* stream)
+{
+    if (int rc = check_tensors(grads, count))
+        return rc;
+    REQUIRE(norm_dev && aligned(norm_dev, 8), "norm_dev is NULL or not aligned to 8 bytes");
+    if (apply)
+        REQUIRE(max_norm >= 0.0, "max_norm is negative or NaN");
+    if (apply == 2) {
+        REQUIRE(std::isfinite(lr) && std::isfinite(lam), "lr or lambda is not finite");
+        if (int rc = check_tensors(params, count))
+            return rc;
+        for (int64_t i = 0; i < count; ++i)
+            REQUIRE(params[i].n == grads[i].n && params[i].dtype == grads[i].dtype,
+                    "a parameter and its gradient differ in size or dtype");
+    }
+    if (int rc = check_work(work, bytes, norm_bytes(count)))
+        return rc;
+    if (apply) {
+        std::vector<Span> spans;
+        spans.reserve((size_t)count * 2);
+        add_spans(spans, grads, count, apply == 1);
+        if (apply == 2)
+            add_spans(spans, params, count, true);
+        REQUIRE(!overlap(spans), "tensors that are written overlap others");
+    }
+    std::vector<NormTensor> list((size_t)count);
+    for (int64_t i = 0; i < count; ++i)
+        list[i] = NormTensor{apply == 2 ? params[i].data : grads[i].data, grads[i].data, grads[i].n, grads[i].dtype};
+    return launched(norm_apply(list.data(), count, apply, max_norm, lr, lam, norm_dev, work, (hipStream_t)stream));
+}
+
+} // namespace
+
+extern "C" {
+
+int mfsgd_embed(const void* table, int64_t rows, int64_t ld, int32_t k, int32_t dtype, const int32_t* ids,
+                int64_t ids_stride, int64_t count, float scale, void* out, int64_t ld_out, void* stream)
+{
+    return guarded([&]() -> int {
+        return embed_impl(RowsLaunch{table, rows, ld, k, dtype, ids, ids_stride, count, scale, out, ld_out}, stream);
+    });
+}
+
+int mfsgd_embed_grad(const void* dout, int64_t ld_dout, const int32_t* ids, int64_t ids_stride, int64_t count,
+                     int32_t k, int32_t dtype, float scale, void* dtable, int64_t rows, int64_t ld,
+                     int32_t accumulate, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    return guarded([&]() -> int {
+        return embed_grad_impl(RowsGradLaunch{dout, ld_dout, ids, ids_stride, count, k, dtype, scale, dtable, rows, ld,
+                                              accumulate != 0, nullptr},
+                               workspace, workspace_bytes, stream);
+    });
+}
+
+int mfsgd_embed_grad_workspace(int64_t count, int32_t k, int64_t* bytes)
+{
+    return guarded([&]() -> int {
+        REQUIRE(bytes, "NULL bytes");
+        REQUIRE(count >= 0 && count <= INT32_MAX, "count must be in [0, 2^31-1]");
+        REQUIRE(k >= 1, "k must be at least 1");
+        *bytes = (int64_t)rows_grad_bytes(count, k);
+        return MFSGD_OK;
+    });
+}
+
+int mfsgd_rows(int32_t side, const int32_t* ids, int64_t ids_stride, int64_t count, int32_t k, int32_t dtype,
+               float scale, void* out, int64_t ld_out, void* stream)
+{
+    return guarded([&]() -> int {
+        ModelView v;
+        void* table = nullptr;
+        int64_t rows = 0;
+        if (int rc = table_of(side, k, dtype, v, table, rows))
+            return rc;
+        return embed_impl(RowsLaunch{table, rows, v.KP, k, v.dtype, ids, ids_stride, count, scale, out, ld_out},
+                          stream);
+    });
+}
+
+int mfsgd_add_rows(int32_t side, const void* dout, int64_t ld_dout, const int32_t* ids, int64_t ids_stride,
+                   int64_t count, int32_t k, int32_t dtype, float scale, void* workspace, int64_t workspace_bytes,
+                   void* stream)
+{
+    return guarded([&]() -> int {
+        ModelView v;
+        void* table = nullptr;
+        int64_t rows = 0;
+        if (int rc = table_of(side, k, dtype, v, table, rows))
+            return rc;
+        return embed_grad_impl(RowsGradLaunch{dout, ld_dout, ids, ids_stride, count, k, v.dtype, scale, table, rows,
+                                              v.KP, 1, nullptr},
+                               workspace, workspace_bytes, stream);
+    });
+}
+
+int mfsgd_grad_norm(const mfsgd_tensor* grads, int64_t count, double* norm_dev, void* workspace,
+                    int64_t workspace_bytes, void* stream)
+{
+    return guarded([&]() -> int {
+        return norm_impl(nullptr, grads, count, 0, 0.0f, 0.0f, 0.0, norm_dev, workspace, workspace_bytes, stream);
+    });
+}
+
+int mfsgd_clip_grads(const mfsgd_tensor* grads, int64_t count, double max_norm, double* norm_dev, void* workspace,
+                     int64_t workspace_bytes, void* stream)
+{
+    return guarded([&]() -> int {
+        return norm_impl(nullptr, grads, count, 1, 0.0f, 0.0f, max_norm, norm_dev, workspace, workspace_bytes, stream);
+    });
+}
+
+int mfsgd_sgd_step(const mfsgd_tensor* params, const mfsgd_tensor* grads, int64_t count, float lr, float lambda,
+                   double max_norm, double* norm_dev, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    return guarded([&]() -> int {
+        return norm_impl(params, grads, count, 2, lr, lambda, max_norm, norm_dev, workspace, workspace_bytes, stream);
+    });
+}
+
+int mfsgd_norm_workspace(int64_t count, int64_t* bytes)
+{
+    return guarded([&]() -> int {
+        REQUIRE(bytes, "NULL bytes");
+        REQUIRE(count >= 0 && count <= kMostTensors, "the number of tensors must be in [0, 2^20]");
+        *bytes = (int64_t)norm_bytes(count);
+        return MFSGD_OK;
+    });
+}
+
+} // extern "C"

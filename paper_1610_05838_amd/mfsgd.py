@@ -24,7 +24,8 @@ LIB_PATH = os.path.join(HERE, "libmfsgd.so")
 
 OK, EINVAL, ENOMEM, EHIP, ESTATE, ETIMEOUT, ENUMERIC = 0, -1, -2, -3, -4, -5, -6
 BATCH_HOGWILD, WAVEFRONT, WAVEFRONT_DET, GLOBAL_TABLE = 0, 1, 2, 3
-FP32, FP16 = 0, 1
+FP32, FP16, BF16 = 0, 1, 2  # BF16: the operators alone
+P, Q = 0, 1
 DBG_VISITS, DBG_TRACE, DBG_PLAN_STARTS, DBG_PLAN_ORDER, DBG_TEAM_MAP, DBG_TEAM_SIZES = 1, 2, 3, 4, 5, 6
 DBG_TABLE_STARTS, DBG_TABLE_ORDER, DBG_PRIORITY = 7, 8, 9
 
@@ -72,6 +73,17 @@ def lib():
             "mfsgd_last_error": ([], C.c_char_p),
             "mfsgd_version": ([], C.c_char_p),
         }
+        sig.update({
+            "mfsgd_embed": ([vp, i64, i64, i32, i32, vp, i64, i64, f32, vp, i64, vp], C.c_int),
+            "mfsgd_embed_grad": ([vp, i64, vp, i64, i64, i32, i32, f32, vp, i64, i64, i32, vp, i64, vp], C.c_int),
+            "mfsgd_embed_grad_workspace": ([i64, i32, C.POINTER(i64)], C.c_int),
+            "mfsgd_rows": ([i32, vp, i64, i64, i32, i32, f32, vp, i64, vp], C.c_int),
+            "mfsgd_add_rows": ([i32, vp, i64, vp, i64, i64, i32, i32, f32, vp, i64, vp], C.c_int),
+            "mfsgd_grad_norm": ([vp, i64, vp, vp, i64, vp], C.c_int),
+            "mfsgd_clip_grads": ([vp, i64, C.c_double, vp, vp, i64, vp], C.c_int),
+            "mfsgd_sgd_step": ([vp, vp, i64, f32, f32, C.c_double, vp, vp, i64, vp], C.c_int),
+            "mfsgd_norm_workspace": ([i64, C.POINTER(i64)], C.c_int),
+        })
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
             fn.argtypes = args
@@ -273,6 +285,221 @@ def debug_priority(s: int, stream=None):
     _check(lib().mfsgd_debug_read(DBG_PRIORITY, C.c_void_p(out.data_ptr()), s * s, _stream(stream)),
            "mfsgd_debug_read")
     return out
+
+
+# --- operators on tables, gradients (see the header for what each computes) ---
+#
+# Outputs and workspaces not passed in are allocated on the stream the work runs
+# on.  Row-major matrices may have any row pitch; a tensor on another device
+# than the current one, of another dtype than its call's or with strided
+# columns is refused before anything is enqueued.
+
+_DTYPES = {torch.float32: FP32, torch.float16: FP16, torch.bfloat16: BF16}
+
+
+class _On:
+    """The stream of a call: its handle, and allocations that belong to it."""
+
+    __slots__ = ("device", "stream", "handle")
+
+    def __init__(self, stream):
+        self.device = torch.cuda.current_device()
+        if stream is not None and stream.device_index != self.device:
+            raise ValueError("the stream is on another device than the current one")
+        self.stream = stream
+        self.handle = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+    def empty(self, shape, dtype):
+        if self.stream is None:
+            return torch.empty(shape, dtype=dtype, device="cuda")
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device="cuda")
+
+    def workspace(self, nbytes):
+        """(address, bytes, tensor) of a new workspace; the tensor must outlive the call."""
+        if not nbytes:
+            return None, 0, None
+        t = self.empty((nbytes,), torch.uint8)
+        return t.data_ptr(), nbytes, t
+
+
+def _matrix(t, what, device, dtype=None, shape=None):
+    """Row pitch of a matrix, after checking it."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.get_device() != device or t.dtype not in _DTYPES:
+        raise TypeError(f"{what} must be a float32, float16 or bfloat16 matrix on the current GPU")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
+    rows, width = t.shape
+    if shape is not None and (rows, width) != shape:
+        raise ValueError(f"{what} must have the shape {shape}, not {(rows, width)}")
+    ld, col = t.stride()
+    if width > 1 and col != 1 or rows > 1 and ld < width:
+        raise ValueError(f"the rows of {what} must be contiguous and not overlap")
+    return ld if rows > 1 and ld >= width else max(width, 1)
+
+
+def _ids(t, device):
+    """Address, stride and length of an id vector."""
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or t.dim() != 1 or t.get_device() != device:
+        raise TypeError("ids must be an int32 vector on the current GPU")
+    n = t.shape[0]
+    stride = t.stride(0) if n > 1 else 1
+    if stride < 1:
+        raise ValueError("ids must have a positive stride")
+    return t.data_ptr(), stride, n
+
+
+def _grad_workspace(on, count, k):
+    n = C.c_int64()
+    _check(lib().mfsgd_embed_grad_workspace(count, k, C.byref(n)), "mfsgd_embed_grad_workspace")
+    return on.workspace(n.value)
+
+
+def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out=None, stream=None) -> torch.Tensor:
+    """Rows of `table` by id, times `scale`; zeros where an id is outside the
+    table (padding).  `ids` may be a column of a sample tensor."""
+    on = _On(stream)
+    ld = _matrix(table, "table", on.device)
+    idp, stride, count = _ids(ids, on.device)
+    rows, k = table.shape
+    if out is None:
+        out = on.empty((count, k), table.dtype)
+        ld_out = k
+    else:
+        ld_out = _matrix(out, "out", on.device, table.dtype, (count, k))
+    _check(lib().mfsgd_embed(table.data_ptr(), rows, ld, k, _DTYPES[table.dtype], idp, stride, count, scale,
+                             out.data_ptr(), ld_out, on.handle), "mfsgd_embed")
+    return out
+
+
+def embed_grad(dout: torch.Tensor, ids: torch.Tensor, rows: int, scale: float = 1.0, out=None,
+               accumulate: bool = False, stream=None) -> torch.Tensor:
+    """The gradient of ``embed`` with respect to its table of `rows` rows: row r
+    is `scale` times the sum of dout's rows whose id is r.  With `accumulate` it
+    is added to `out`, of which only those rows are touched."""
+    on = _On(stream)
+    ld = _matrix(dout, "dout", on.device)
+    idp, stride, count = _ids(ids, on.device)
+    n, k = dout.shape
+    if n != count:
+        raise ValueError(f"dout has {n} rows for {count} ids")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs an `out` to add to")
+        out = on.empty((rows, k), dout.dtype)
+        ld_out = k
+    else:
+        ld_out = _matrix(out, "out", on.device, dout.dtype, (rows, k))
+    work, nbytes, keep = _grad_workspace(on, count, k)
+    _check(lib().mfsgd_embed_grad(dout.data_ptr(), ld, idp, stride, count, k, _DTYPES[dout.dtype], scale,
+                                  out.data_ptr(), rows, ld_out, accumulate, work, nbytes, on.handle),
+           "mfsgd_embed_grad")
+    return out
+
+
+def rows(side: int, ids: torch.Tensor, k: int, dtype=None, scale: float = 1.0, out=None,
+         stream=None) -> torch.Tensor:
+    """``embed`` on the model's own factors: `side` is P (users) or Q (items).
+    k and dtype must be the model's (dtype by default: what option "dtype" says)."""
+    on = _On(stream)
+    idp, stride, count = _ids(ids, on.device)
+    dtype = dtype or _storage_dtype()
+    if out is None:
+        out = on.empty((count, k), dtype)
+        ld_out = k
+    else:
+        ld_out = _matrix(out, "out", on.device, dtype, (count, k))
+    _check(lib().mfsgd_rows(side, idp, stride, count, k, _DTYPES[dtype], scale, out.data_ptr(), ld_out, on.handle),
+           "mfsgd_rows")
+    return out
+
+
+def add_rows(side: int, dout: torch.Tensor, ids: torch.Tensor, scale: float, stream=None) -> None:
+    """Adds `scale` times the sum of dout's rows of every id to that row of the
+    model's factors, in place: the gradient step of those rows at scale = -lr.
+    dout has the model's k and dtype."""
+    on = _On(stream)
+    ld = _matrix(dout, "dout", on.device)
+    idp, stride, count = _ids(ids, on.device)
+    n, k = dout.shape
+    if n != count:
+        raise ValueError(f"dout has {n} rows for {count} ids")
+    work, nbytes, keep = _grad_workspace(on, count, k)
+    _check(lib().mfsgd_add_rows(side, dout.data_ptr(), ld, idp, stride, count, k, _DTYPES[dout.dtype], scale, work,
+                                nbytes, on.handle), "mfsgd_add_rows")
+
+
+class TensorList:
+    """Tensors that ``grad_norm``, ``clip_grads`` and ``sgd_step`` take together,
+    checked and laid out once.  It holds the tensors: they must keep the storage
+    they had (not be moved, resized or set to another) while it is used."""
+
+    class _Entry(C.Structure):
+        _fields_ = [("data", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32), ("unused", C.c_int32)]
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.device = None
+        self.entries = (TensorList._Entry * max(len(self.tensors), 1))()
+        for i, t in enumerate(self.tensors):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in _DTYPES or not t.is_contiguous():
+                raise TypeError("the tensors must be contiguous float32, float16 or bfloat16 tensors on the GPU")
+            if self.device is None:
+                self.device = t.get_device()
+            if t.get_device() != self.device:
+                raise ValueError("the tensors must be on one device")
+            self.entries[i].data, self.entries[i].n = t.data_ptr(), t.numel()
+            self.entries[i].dtype = _DTYPES[t.dtype]
+        n = C.c_int64()
+        _check(lib().mfsgd_norm_workspace(len(self.tensors), C.byref(n)), "mfsgd_norm_workspace")
+        self.workspace_bytes = n.value
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _tensor_list(tensors, on):
+    a = tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+    if a.device is not None and a.device != on.device:
+        raise ValueError("the tensors are on another device than the current one")
+    return a
+
+
+def grad_norm(grads, stream=None) -> torch.Tensor:
+    """The norm of all gradients together (a TensorList or an iterable of
+    tensors): a float64 scalar on the GPU."""
+    on = _On(stream)
+    g = _tensor_list(grads, on)
+    norm = on.empty((), torch.float64)
+    work, nbytes, keep = on.workspace(g.workspace_bytes)
+    _check(lib().mfsgd_grad_norm(g.entries, len(g), norm.data_ptr(), work, nbytes, on.handle), "mfsgd_grad_norm")
+    return norm
+
+
+def clip_grads(grads, max_norm: float, stream=None) -> torch.Tensor:
+    """Scales all gradients in place so that their norm is at most `max_norm`;
+    returns the norm they had."""
+    on = _On(stream)
+    g = _tensor_list(grads, on)
+    norm = on.empty((), torch.float64)
+    work, nbytes, keep = on.workspace(g.workspace_bytes)
+    _check(lib().mfsgd_clip_grads(g.entries, len(g), max_norm, norm.data_ptr(), work, nbytes, on.handle),
+           "mfsgd_clip_grads")
+    return norm
+
+
+def sgd_step(params, grads, lr: float, lam: float = 0.0, max_norm: float = float("inf"), stream=None) -> torch.Tensor:
+    """p <- p - lr (c g + lam p) with c = min(1, max_norm / norm of all
+    gradients), in place; the gradients stay.  Returns the norm."""
+    on = _On(stream)
+    p, g = _tensor_list(params, on), _tensor_list(grads, on)
+    if len(p) != len(g):
+        raise ValueError(f"{len(p)} parameters and {len(g)} gradients")
+    norm = on.empty((), torch.float64)
+    work, nbytes, keep = on.workspace(g.workspace_bytes)
+    _check(lib().mfsgd_sgd_step(p.entries, g.entries, len(g), lr, lam, max_norm, norm.data_ptr(), work, nbytes,
+                                on.handle), "mfsgd_sgd_step")
+    return norm
 
 
 def finalize() -> None:

@@ -1,0 +1,283 @@
+"""Row lookups and their gradient (mfsgd_embed, mfsgd_embed_grad, and the two on
+the model's factors) against their definition in 64 bits.
+
+Gradients are mostly tested on small integers, whose sums binary32 holds
+exactly whatever their order: the result then has to be the exact sum, rounded
+once.  eps / 2 of a type is the largest relative error of one rounding."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+from paper_1610_05838_amd import mfsgd as M  # noqa: E402
+
+DTYPES = (torch.float32, torch.float16, torch.bfloat16)
+ID = {torch.float32: "fp32", torch.float16: "fp16", torch.bfloat16: "bf16"}
+
+
+def rng(seed):
+    return torch.Generator("cuda").manual_seed(seed)
+
+
+def pitched(rows, k, ld, dtype, fill=0.0, shift=0):
+    """A rows x k view of pitch ld that starts `shift` elements into its storage, and the whole storage."""
+    store = torch.full((shift + rows * ld + 16,), fill, dtype=dtype, device="cuda")
+    return store[shift:shift + rows * ld].view(rows, ld)[:, :k] if rows else store[:0].view(0, k), store
+
+
+def once(x64, dtype):
+    """x64 rounded once (binary64 to binary32 to a 16-bit type would round twice: not for these exact sums)."""
+    return x64.to(dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
+@pytest.mark.parametrize("k", [1, 2, 3, 4, 5, 7, 8, 9, 31, 64, 100, 127, 128, 257, 500, 1025])
+def test_embed(dtype, k):
+    for count, rows, ld, shift, stride, scale in ((0, 3, k, 0, 1, 1.0), (1, 1, k, 0, 1, 1.0), (63, 5, k + 3, 1, 3, 1.0),
+                                                  (1000, 700, k, 3, 2, 22.627417), (1, 9, k + 1, 0, 3, 0.25)):
+        g = rng(k * 7 + count)
+        table, _ = pitched(rows, k, ld, dtype, shift=shift)
+        table.copy_(torch.randn(rows, k, generator=g, device="cuda"))
+        ids = torch.randint(-2, rows + 2, (max(count, 1), stride), generator=g, device="cuda", dtype=torch.int32)[:count, 0]
+        if count > 10:
+            ids[3], ids[4] = -2**31, 2**31 - 1
+        out, store = pitched(count, k, ld + 2, dtype, fill=7.0, shift=shift)
+        before = store.clone()
+        got = M.embed(table, ids, scale=scale, out=out)
+        assert got is out
+        there = (ids >= 0) & (ids < rows)
+        want = torch.where(there[:, None], table[torch.where(there, ids, 0).long()].double(), 0.0)
+        want = want * float(np.float32(scale))
+        # the product is rounded to binary32, then to the type
+        eps = torch.finfo(dtype).eps / 2
+        tol = want.abs() * (eps + 2.0**-24) * (1 + 2.0**-8) + torch.finfo(dtype).smallest_normal * eps
+        assert bool(((out.double() - want).abs() <= tol).all())
+        if scale == 1.0:
+            assert torch.equal(out.double(), want)
+        # nothing but the k columns of the rows was written
+        out.fill_(7.0)
+        assert torch.equal(store, before)
+        if stride == 1 and count:
+            assert torch.equal(M.embed(table, ids, scale=scale).double(), M.embed(table, ids.clone(), scale).double())
+
+
+def test_embed_padding_reads_no_row():
+    """Ids outside the table give zeros, whatever the table holds."""
+    table = torch.full((4, 40), float("nan"), device="cuda")
+    out = M.embed(table, torch.tensor([-1, 4, 2**31 - 1], dtype=torch.int32, device="cuda"), scale=3.0)
+    assert torch.equal(out, torch.zeros(3, 40, device="cuda"))
+
+
+def grad_want(dout, ids, rows, scale):
+    there = (ids >= 0) & (ids < rows)
+    want = torch.zeros(rows, dout.shape[1], dtype=torch.float64, device="cuda")
+    want.index_add_(0, ids[there].long(), dout[there].double())
+    return want * scale
+
+
+def make_ids(kind, count, rows, g):
+    if kind == "uniform":
+        return torch.randint(0, rows, (count,), generator=g, device="cuda", dtype=torch.int32)
+    if kind == "same":
+        return torch.full((count,), rows // 2, dtype=torch.int32, device="cuda")
+    if kind == "sorted":
+        return torch.randint(0, rows, (count,), generator=g, device="cuda", dtype=torch.int32).sort()[0]
+    if kind == "none":
+        return torch.where(torch.arange(count, device="cuda") % 2 == 0, -1, rows).int()
+    u = torch.rand(count, generator=g, device="cuda", dtype=torch.float64)  # skewed, some padding
+    ids = (torch.exp(u * np.log(rows + 1.0)) - 1).long().clamp_(0, rows - 1)
+    ids = torch.randperm(rows, generator=g, device="cuda")[ids].int()
+    ids[torch.rand(count, generator=g, device="cuda") < 0.1] = -1
+    return ids
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
+@pytest.mark.parametrize("kind", ["uniform", "same", "sorted", "none", "skewed"])
+@pytest.mark.parametrize("count,rows,k", [(1, 1, 1), (5, 7, 3), (64, 300, 33), (65, 2, 128), (1000, 257, 100),
+                                          (4096, 50, 64), (4097, 70_001, 5), (5000, 255, 130), (9_999, 256, 1100),
+                                          (70_000, 1, 2), (70_000, 5000, 257), (140_000, 300, 64)])
+def test_embed_grad_is_the_exact_sum(dtype, kind, count, rows, k):
+    g = rng(count + rows)
+    dout, _ = pitched(count, k, k + 1, dtype, shift=1)
+    dout.copy_(torch.randint(-4, 5, (count, k), generator=g, device="cuda").to(dtype))
+    # the largest sum stays below 2^24 (and below binary16's largest value, rounded once)
+    ids = make_ids(kind, count, rows, g)
+    want = grad_want(dout, ids, rows, 0.125)
+    out, store = pitched(rows, k, k + 3, dtype, fill=5.0)
+    before = store.clone()
+    M.embed_grad(dout, ids, rows, scale=0.125, out=out)
+    assert torch.equal(out, once(want, dtype))
+    out.fill_(5.0)
+    assert torch.equal(store, before)  # nothing beside the table's columns
+    # added to a table of integers: rows without a token keep their bits
+    base = torch.randint(-8, 9, (rows, k), generator=g, device="cuda").to(dtype)
+    out.copy_(base)
+    M.embed_grad(dout, ids, rows, scale=0.125, out=out, accumulate=True)
+    assert torch.equal(out, once(base.double() + want, dtype))
+
+
+def test_embed_grad_long_rows():
+    """One row's tokens over hundreds of tiles, another's over a few, padding between."""
+    count, rows, k = 400_000, 3, 70
+    g = rng(11)
+    dout = torch.randint(-3, 4, (count, k), generator=g, device="cuda").float()
+    ids = torch.randint(0, 100, (count,), generator=g, device="cuda", dtype=torch.int32)
+    ids = torch.where(ids < 97, 1, torch.where(ids == 97, 0, torch.where(ids == 98, 2, -1))).int()
+    got = M.embed_grad(dout, ids, rows)
+    assert torch.equal(got.double(), grad_want(dout, ids, rows, 1.0))
+
+
+@pytest.mark.parametrize("count", [900, 60_000])
+def test_embed_grad_rounding_and_repeat(count):
+    """Random values: n terms added in binary32 are off by at most (n - 1) 2^-24 of the sum of their
+    magnitudes, the scale by 2^-24 more; the same call gives the same bits."""
+    rows, k = 40, 96
+    g = rng(count)
+    for dtype in DTYPES:
+        dout = torch.randn(count, k, generator=g, device="cuda").to(dtype)
+        ids = make_ids("skewed", count, rows, g)
+        got = M.embed_grad(dout, ids, rows, scale=0.3)
+        s = float(np.float32(0.3))
+        want, mag = grad_want(dout, ids, rows, s), grad_want(dout.abs(), ids, rows, s)
+        n = torch.bincount(ids[ids >= 0].long(), minlength=rows).double()[:, None]
+        tol = mag * (n + 1) * 2.0**-24 * 1.01 + want.abs() * torch.finfo(dtype).eps / 2 * 1.01 + 1e-7
+        assert bool(((got.double() - want).abs() <= tol).all())
+        for _ in range(3):
+            assert torch.equal(got, M.embed_grad(dout, ids, rows, scale=0.3))
+
+
+@pytest.mark.parametrize("count", [300, 6000])
+def test_embed_grad_leaves_padding_out(count):
+    """What stands in a padded token's row reaches nothing, NaN and infinity included."""
+    g = rng(5)
+    dout = torch.randint(-4, 5, (count, 48), generator=g, device="cuda").float()
+    ids = make_ids("uniform", count, 50, g)
+    ids[::3] = -1
+    ids[1::7] = 50
+    want = grad_want(dout, ids, 50, 1.0)
+    dout[(ids < 0) | (ids >= 50)] = float("nan")
+    dout[0] = float("inf")
+    assert torch.equal(M.embed_grad(dout, ids, 50).double(), want)
+
+
+def test_embed_grad_is_the_lookups_derivative():
+    """<dout, embed(T + h D) - embed(T - h D)> / 2h = <embed_grad(dout), D>: exact for a linear map on these values."""
+    g = rng(3)
+    T = torch.randint(-8, 9, (30, 20), generator=g, device="cuda").float()
+    D = torch.randint(-2, 3, (30, 20), generator=g, device="cuda").float()
+    ids = make_ids("skewed", 500, 30, g)
+    dout = torch.randint(-2, 3, (500, 20), generator=g, device="cuda").float()
+    diff = (M.embed(T + D, ids, 0.5).double() - M.embed(T - D, ids, 0.5).double()) / 2
+    assert float((dout.double() * diff).sum()) == float((M.embed_grad(dout, ids, 30, 0.5).double() * D.double()).sum())
+
+
+def test_offsets_past_32_bits():
+    """Rows beyond 2^31 elements of a table (binary16, 4.8 GB)."""
+    rows, k = 37_500_001, 64
+    table = torch.zeros(rows, k, dtype=torch.float16, device="cuda")
+    ids = torch.tensor([rows - 1, 33_554_432, 0, rows - 2, -1, rows - 1], dtype=torch.int32, device="cuda")
+    for j, i in enumerate(ids.tolist()):
+        if i >= 0:
+            table[i] = float(j + 1)
+    out = M.embed(table, ids)
+    assert out[:, 0].tolist() == [6.0, 2.0, 3.0, 4.0, 0.0, 6.0]
+    dout = torch.ones(6, k, dtype=torch.float16, device="cuda")
+    M.embed_grad(dout, ids, rows, scale=2.0, out=table, accumulate=True)
+    assert table[ids[:4].long(), 63].tolist() == [10.0, 4.0, 5.0, 6.0]
+    many = ids.repeat(2000)
+    M.embed_grad(dout.repeat(2000, 1), many, rows, scale=0.5, out=table)
+    assert table[ids[:4].long(), 63].tolist() == [2000.0, 1000.0, 1000.0, 1000.0]
+    assert int(torch.count_nonzero(table[::, 0])) == 4
+
+
+def test_streams_and_graphs():
+    """On another stream, and captured: every replay sees the inputs as they are then."""
+    g = rng(9)
+    ids = make_ids("skewed", 6000, 500, g)
+    dout = torch.randint(-4, 5, (6000, 40), generator=g, device="cuda").float()
+    table = torch.randint(-4, 5, (500, 40), generator=g, device="cuda").float()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    a = M.embed_grad(dout, ids, 500, stream=side)
+    b = M.embed(table, ids, stream=side)
+    side.synchronize()
+    assert torch.equal(a.double(), grad_want(dout, ids, 500, 1.0)) and torch.equal(b, M.embed(table, ids))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        few = M.embed_grad(dout[:100], ids[:100], 500)
+        many = M.embed_grad(dout, ids, 500)
+        rows = M.embed(table, ids, scale=2.0)
+    for step in range(4):
+        ids.copy_(make_ids("skewed" if step % 2 else "same", 6000, 500, g))
+        dout.copy_(torch.randint(-4, 5, (6000, 40), generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(few.double(), grad_want(dout[:100], ids[:100], 500, 1.0))
+        assert torch.equal(many.double(), grad_want(dout, ids, 500, 1.0))
+        assert torch.equal(rows, M.embed(table, ids, scale=2.0))
+        assert torch.equal(many, M.embed_grad(dout, ids, 500))  # eager between the replays
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("k", [32, 100])
+def test_model_rows(dtype, k):
+    """The same on the library's own factors, whose rows are padded inside."""
+    m, n = 3000, 700
+    M.reset_options()
+    M.set_option("dtype", dtype)
+    M.init(m, n, k, 5)
+    P, Q = M.get_factors(m, n, k)
+    g = rng(dtype * 10 + k)
+    for side, table in ((M.P, P), (M.Q, Q)):
+        rows = table.shape[0]
+        for count in (1, 700, 9000):
+            ids = make_ids("skewed", count, rows, g)
+            assert torch.equal(M.rows(side, ids, k, scale=1.5), M.embed(table, ids, scale=1.5))
+            dout = torch.randn(count, k, generator=g, device="cuda").to(table.dtype)
+            M.add_rows(side, dout, ids, -0.01)
+            M.embed_grad(dout, ids, rows, scale=-0.01, out=table, accumulate=True)
+    P2, Q2 = M.get_factors(m, n, k)
+    assert torch.equal(P, P2) and torch.equal(Q, Q2)
+    for bad in (dict(side=2), dict(k=k + 1), dict(dtype=torch.bfloat16)):
+        with pytest.raises(M.MfsgdError) as e:
+            M.rows(**{**dict(side=M.P, ids=ids, k=k, dtype=P.dtype), **bad})
+        assert e.value.code == M.EINVAL
+    # an option set after init does not change what the model holds
+    M.set_option("dtype", 1 - dtype)
+    with pytest.raises(M.MfsgdError):
+        M.rows(M.P, ids, k)
+    M.reset_options()
+    M.finalize()
+
+
+def test_binding_refuses():
+    t = torch.zeros(4, 8, device="cuda")
+    ids = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for bad in (t.cpu(), t.double(), t[0], [1]):
+        with pytest.raises(TypeError):
+            M.embed(bad, ids)
+    for bad in (ids.long(), ids.cpu(), t, ids[:0].view(0, 1)):
+        with pytest.raises(TypeError):
+            M.embed(t, bad)
+    with pytest.raises(ValueError):
+        M.embed(t.t(), ids)
+    with pytest.raises(ValueError):
+        M.embed(t[:1].expand(4, 8), ids)
+    with pytest.raises(ValueError):
+        M.embed(t, ids, out=torch.zeros(2, 8, device="cuda"))
+    with pytest.raises(TypeError):
+        M.embed(t, ids, out=torch.zeros(3, 8, dtype=torch.float16, device="cuda"))
+    with pytest.raises(ValueError):
+        M.embed_grad(t, ids, 10)
+    with pytest.raises(ValueError):
+        M.embed_grad(t[:3], ids, 10, accumulate=True)
+    with pytest.raises(ValueError):
+        M.embed_grad(t[:3], ids, 10, out=torch.zeros(9, 8, device="cuda"))
+    with pytest.raises(ValueError):
+        M.embed(t, ids[:1].expand(3))
+    with pytest.raises(M.MfsgdError):
+        M.embed(t[:0], ids)

@@ -1,0 +1,148 @@
+"""What the operators of include/mfsgd.h refuse, through the C ABI and without a
+GPU: every argument that a kernel could not take safely is turned away before
+anything is enqueued, with a text that says why."""
+import ctypes as C
+import os
+
+import pytest
+
+from paper_1610_05838_amd import mfsgd as M
+
+EINVAL, ESTATE = -1, -4
+A = 0x10000  # an aligned address that no refused call may touch
+BIG = 1 << 62
+INT32_MAX = 2**31 - 1
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(M.LIB_PATH):
+        from paper_1610_05838_amd import _build
+        _build.build()
+    return M.lib()
+
+
+def refused(lib, fn, args, code=EINVAL):
+    assert getattr(lib, fn)(*args) == code, (fn, args)
+    assert lib.mfsgd_last_error(), fn
+
+
+def changed(base, **what):
+    got = dict(base)
+    got.update(what)
+    return tuple(got.values())
+
+
+EMBED = dict(table=A, rows=10, ld=8, k=8, dtype=0, ids=A, ids_stride=1, count=4, scale=1.0, out=A, ld_out=8,
+             stream=None)
+GRAD = dict(dout=A, ld_dout=8, ids=A, ids_stride=1, count=4, k=8, dtype=0, scale=1.0, dtable=A, rows=10, ld=8,
+            accumulate=0, work=None, nbytes=0, stream=None)
+
+
+@pytest.mark.parametrize("what", [
+    dict(table=None), dict(table=A + 2), dict(rows=0), dict(rows=-1), dict(rows=2**31), dict(ld=7), dict(k=0),
+    dict(k=-3), dict(dtype=3), dict(dtype=-1), dict(ids=None), dict(ids=A + 1), dict(ids_stride=0),
+    dict(ids_stride=-1), dict(count=-1), dict(count=2**31), dict(out=None), dict(out=A + 1), dict(ld_out=7),
+    dict(ld=BIG), dict(dtype=1, table=A + 1)])
+def test_embed_refuses(lib, what):
+    refused(lib, "mfsgd_embed", changed(EMBED, **what))
+
+
+@pytest.mark.parametrize("what", [
+    dict(dout=None), dict(dout=A + 2), dict(ld_dout=7), dict(ids=None), dict(ids=A + 2), dict(ids_stride=0),
+    dict(count=-1), dict(count=2**31), dict(k=0), dict(dtype=9), dict(dtable=None), dict(dtable=A + 1),
+    dict(rows=0), dict(rows=2**31), dict(ld=3),
+    dict(count=100_000, work=None, nbytes=BIG), dict(count=100_000, work=A, nbytes=64),
+    dict(count=100_000, work=A + 8, nbytes=BIG), dict(count=100_000, work=A, nbytes=-1)])
+def test_embed_grad_refuses(lib, what):
+    refused(lib, "mfsgd_embed_grad", changed(GRAD, **what))
+
+
+def test_empty_calls_are_no_errors(lib):
+    """No tokens: nothing to read or write (the gradient only where it adds)."""
+    assert lib.mfsgd_embed(*changed(EMBED, count=0, ids=None, out=None)) == 0
+    assert lib.mfsgd_embed_grad(*changed(GRAD, count=0, ids=None, dout=None, accumulate=1)) == 0
+    assert lib.mfsgd_last_error() == b""
+
+
+def test_embed_grad_workspace(lib):
+    n = C.c_int64(-1)
+    assert lib.mfsgd_embed_grad_workspace(10, 128, C.byref(n)) == 0 and n.value == 0
+    assert lib.mfsgd_embed_grad_workspace(1_000_000, 128, C.byref(n)) == 0 and n.value >= 16_000_000
+    assert lib.mfsgd_embed_grad_workspace(INT32_MAX, 1 << 20, C.byref(n)) == 0 and n.value > 1 << 45
+    for count, k in ((-1, 8), (2**31, 8), (5, 0)):
+        refused(lib, "mfsgd_embed_grad_workspace", (count, k, C.byref(n)))
+    refused(lib, "mfsgd_embed_grad_workspace", (5, 8, None))
+
+
+def test_model_rows_need_a_model(lib):
+    assert lib.mfsgd_finalize() in (0, -3)
+    refused(lib, "mfsgd_rows", (0, A, 1, 4, 8, 0, 1.0, A, 8, None), ESTATE)
+    refused(lib, "mfsgd_add_rows", (0, A, 8, A, 1, 4, 8, 0, 1.0, None, 0, None), ESTATE)
+
+
+def entries(*ts):
+    a = (M.TensorList._Entry * max(len(ts), 1))()
+    for e, (p, n, d) in zip(a, ts):
+        e.data, e.n, e.dtype = p, n, d
+    return a
+
+
+GOOD = (A, 100, 0)
+
+
+@pytest.mark.parametrize("t", [(None, 5, 0), (A + 2, 5, 0), (A + 1, 5, 1), (A, -1, 0), (A, (1 << 40) + 1, 0), (A, 5, 3),
+                               (A, 5, -1)])
+def test_norm_refuses_a_tensor(lib, t):
+    a = entries(GOOD, t)
+    refused(lib, "mfsgd_grad_norm", (a, 2, A, A, BIG, None))
+    refused(lib, "mfsgd_clip_grads", (a, 2, 1.0, A, A, BIG, None))
+    refused(lib, "mfsgd_sgd_step", (a, a, 2, 0.1, 0.0, 1.0, A, A, BIG, None))
+
+
+@pytest.mark.parametrize("call", [
+    dict(count=-1), dict(count=(1 << 20) + 1), dict(list=None), dict(norm=None), dict(norm=A + 4), dict(work=None),
+    dict(work=A + 8), dict(nbytes=100), dict(nbytes=-1)])
+def test_norm_refuses(lib, call):
+    base = dict(list=entries(GOOD), count=1, norm=A, work=A, nbytes=BIG, stream=None)
+    refused(lib, "mfsgd_grad_norm", changed(base, **call))
+
+
+def test_norm_refuses_too_many_elements(lib):
+    a = entries(*[(A, 1 << 40, 1)] * 9)
+    refused(lib, "mfsgd_grad_norm", (a, 9, A, A, BIG, None))
+
+
+@pytest.mark.parametrize("max_norm", [-1.0, float("nan")])
+def test_clip_refuses_a_bound(lib, max_norm):
+    refused(lib, "mfsgd_clip_grads", (entries(GOOD), 1, max_norm, A, A, BIG, None))
+
+
+def test_clip_refuses_overlap(lib):
+    for b in ((A, 100, 0), (A + 396, 10, 0), (A + 200, 1, 1), (A - 4, 2, 0)):
+        refused(lib, "mfsgd_clip_grads", (entries(GOOD, b), 2, 1.0, A, A, BIG, None))
+        refused(lib, "mfsgd_clip_grads", (entries(b, GOOD), 2, 1.0, A, A, BIG, None))
+    # inside one that a later one follows
+    refused(lib, "mfsgd_clip_grads", (entries((A, 1000, 0), (A + 400, 10, 0), (A + 3000, 10, 0)), 3, 1.0, A, A, BIG,
+                                      None))
+
+
+def test_step_refuses(lib):
+    g = (A + 4096, 100, 0)
+    for p in ((A, 99, 0), (A, 100, 1), (A + 4096, 100, 0), (A + 4092, 100, 0), (A + 3700, 100, 0)):
+        refused(lib, "mfsgd_sgd_step", (entries(p), entries(g), 1, 0.1, 0.0, 1.0, A, A, BIG, None))
+    for lr, lam, most in ((float("inf"), 0.0, 1.0), (float("nan"), 0.0, 1.0), (0.1, float("inf"), 1.0),
+                          (0.1, 0.0, -2.0), (0.1, 0.0, float("nan"))):
+        refused(lib, "mfsgd_sgd_step", (entries(GOOD), entries(g), 1, lr, lam, most, A, A, BIG, None))
+    # one parameter twice
+    refused(lib, "mfsgd_sgd_step", (entries(GOOD, GOOD), entries(g, g), 2, 0.1, 0.0, 1.0, A, A, BIG, None))
+
+
+def test_norm_workspace(lib):
+    n = C.c_int64(-1)
+    assert lib.mfsgd_norm_workspace(0, C.byref(n)) == 0 and n.value > 0
+    a = n.value
+    assert lib.mfsgd_norm_workspace(1000, C.byref(n)) == 0 and n.value > a
+    for count in (-1, (1 << 20) + 1):
+        refused(lib, "mfsgd_norm_workspace", (count, C.byref(n)))
+    refused(lib, "mfsgd_norm_workspace", (1, None))
