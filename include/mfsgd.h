@@ -543,6 +543,48 @@ int mfsgd_add_rows(int32_t side, const void* dout, int64_t ld_dout, const int32_
                    void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Matrix products with bias, activation and residual; conventions as for the
+ * operators above.
+ *   Z = X W^T + bias,   Y = act(Z) + residual
+ * X is M x K, W N x K (a row per output, as Q has a row per item), Y, Z and
+ * residual M x N, bias N values (contiguous).  bias, residual and z may be NULL:
+ * left out.  z receives the pre-activation for the gradient.  The epilogue works
+ * on the binary32 sums; Z and Y are each rounded once.  residual may be y itself
+ * (same pointer and ld).  Any M, N, K in [0, 2^31-1] (K = 0: Z = bias). */
+enum {
+    MFSGD_ACT_NONE = 0,    /* Z */
+    MFSGD_ACT_RELU = 1,    /* max(Z, 0) */
+    MFSGD_ACT_SIGMOID = 2, /* 1 / (1 + exp(-Z)) */
+    MFSGD_ACT_SILU = 3,    /* Z / (1 + exp(-Z)) */
+    MFSGD_ACT_GELU = 4     /* Z (1 + erf(Z / sqrt 2)) / 2 */
+};
+int mfsgd_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, const void* residual,
+                 int64_t ldr, int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t act, void* y, int64_t ldy,
+                 void* z, int64_t ldz, void* workspace, int64_t workspace_bytes, void* stream);
+int mfsgd_linear_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, int64_t* bytes);
+
+/* Its gradient: for dY (M x N) and the kept Z,
+ *   dZ = dY * act'(Z) elementwise,   dX = dZ W,   dW = dZ^T X,   dbias = column sums of dZ
+ * (the residual's gradient is dY).  dx, dw and dbias may be NULL: left out; z may
+ * be NULL for MFSGD_ACT_NONE; w may be NULL without dx, x without dw.  The slope
+ * of relu at 0 is 0.  dZ is rounded to the dtype before the products (as the
+ * matrix instructions take it) and summed unrounded into dbias. */
+int mfsgd_linear_grad(const void* dy, int64_t lddy, const void* z, int64_t ldz, const void* x, int64_t ldx,
+                      const void* w, int64_t ldw, int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t act,
+                      void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+int mfsgd_linear_grad_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, int64_t* bytes);
+
+/* The model's answer: the scores of `count` users against all its items,
+ *   out[i, v] = act(p_{users[i]} . q_v + bias[v])
+ * (after mfsgd_init, on its device; k, n and dtype must be the model's).  bias (n
+ * values) may be NULL.  A user outside [0, m) stands for none: act(bias). */
+int mfsgd_scores(const int32_t* users, int64_t users_stride, int64_t count, int64_t n, int32_t dtype,
+                 const void* bias, int32_t act, void* out, int64_t ld_out, void* workspace, int64_t workspace_bytes,
+                 void* stream);
+int mfsgd_scores_workspace(int64_t count, int64_t* bytes); /* ESTATE before mfsgd_init */
+
+/* ---------------------------------------------------------------------------
  * The global norm of many gradients, and clipping by it.  Conventions as for
  * the operators above, except that every tensor has a dtype of its own; `list`
  * is HOST memory, read before the call returns.

@@ -19,7 +19,7 @@ INCLUDE = os.path.join(ROOT, "include")
 OBJDIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libmfsgd.so")
 SOURCES = ["mfsgd_api.hip", "mfsgd_aux.hip", "mfsgd_table.hip", "mfsgd_kernels_f32.hip", "mfsgd_kernels_f16.hip",
-           "ops_api.hip", "ops_rows.hip", "ops_norm.hip"]
+           "ops_api.hip", "ops_rows.hip", "ops_norm.hip", "ops_linear.hip"]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -113,6 +113,88 @@ int table_of(int32_t side, int32_t k, int32_t dtype, ModelView& v, void*& table,
     return MFSGD_OK;
 }
 
+// ---- products ----
+
+int check_product(int64_t M, int64_t N, int64_t K, int32_t dtype)
+{
+    REQUIRE(M >= 0 && N >= 0 && K >= 0 && M <= INT32_MAX && N <= INT32_MAX && K <= INT32_MAX,
+            "M, N and K must be in [0, 2^31-1]");
+    REQUIRE(dtype_ok(dtype), "unknown dtype");
+    return MFSGD_OK;
+}
+
+int linear_impl(LinearLaunch a, void* work, int64_t bytes, void* stream)
+{
+    if (int rc = check_product(a.M, a.N, a.K, a.dtype))
+        return rc;
+    REQUIRE(a.act >= MFSGD_ACT_NONE && a.act <= MFSGD_ACT_GELU, "unknown act");
+    REQUIRE(matrix_ok(a.x, a.M, a.K, a.ldx, a.dtype), "x is NULL or misaligned, or ldx is below K");
+    REQUIRE(matrix_ok(a.w, a.N, a.K, a.ldw, a.dtype), "w is NULL or misaligned, or ldw is below K");
+    REQUIRE(aligned(a.bias, elem_bytes(a.dtype)), "bias is misaligned");
+    REQUIRE(!a.residual || matrix_ok(a.residual, a.M, a.N, a.ldr, a.dtype),
+            "residual is misaligned, or ldr is below N");
+    REQUIRE(matrix_ok(a.y, a.M, a.N, a.ldy, a.dtype), "y is NULL or misaligned, or ldy is below N");
+    REQUIRE(!a.z || matrix_ok(a.z, a.M, a.N, a.ldz, a.dtype), "z is misaligned, or ldz is below N");
+    if (int rc = check_work(work, bytes, linear_bytes(a.M, a.N, a.K, a.dtype)))
+        return rc;
+    a.work = work;
+    return launched(linear(a, (hipStream_t)stream));
+}
+
+int linear_grad_impl(LinearGradLaunch a, void* work, int64_t bytes, void* stream)
+{
+    if (int rc = check_product(a.M, a.N, a.K, a.dtype))
+        return rc;
+    REQUIRE(a.act >= MFSGD_ACT_NONE && a.act <= MFSGD_ACT_GELU, "unknown act");
+    REQUIRE(matrix_ok(a.dy, a.M, a.N, a.lddy, a.dtype), "dy is NULL or misaligned, or lddy is below N");
+    REQUIRE(a.act == MFSGD_ACT_NONE || matrix_ok(a.z, a.M, a.N, a.ldz, a.dtype),
+            "z is NULL or misaligned, or ldz is below N");
+    REQUIRE(!a.dw || matrix_ok(a.x, a.M, a.K, a.ldx, a.dtype), "x is NULL or misaligned, or ldx is below K");
+    REQUIRE(!a.dx || matrix_ok(a.w, a.N, a.K, a.ldw, a.dtype), "w is NULL or misaligned, or ldw is below K");
+    REQUIRE(!a.dx || matrix_ok(a.dx, a.M, a.K, a.lddx, a.dtype), "dx is misaligned, or lddx is below K");
+    REQUIRE(!a.dw || matrix_ok(a.dw, a.N, a.K, a.lddw, a.dtype), "dw is misaligned, or lddw is below K");
+    REQUIRE(aligned(a.dbias, elem_bytes(a.dtype)), "dbias is misaligned");
+    if (int rc = check_work(work, bytes, linear_grad_bytes(a.M, a.N, a.K, a.dtype)))
+        return rc;
+    a.work = work;
+    return launched(linear_grad(a, (hipStream_t)stream));
+}
+
+// The model's scores: the users' rows into the workspace, whole (their padding is zero, as the items' is), then the
+// product with Q as it lies.
+size_t scores_rows_bytes(const ModelView& v, int64_t count)
+{
+    return round256((size_t)count * (size_t)v.KP * elem_bytes(v.dtype));
+}
+
+int scores_impl(const int32_t* users, int64_t stride, int64_t count, int64_t n, int32_t dtype, const void* bias,
+                int32_t act, void* out, int64_t ld_out, void* work, int64_t bytes, void* stream)
+{
+    ModelView v;
+    void* P = nullptr;
+    int64_t m = 0;
+    if (!model_view(&v))
+        return set_error(MFSGD_ESTATE, "mfsgd_init has not been called");
+    if (int rc = table_of(MFSGD_P, v.k, dtype, v, P, m))
+        return rc;
+    REQUIRE(n == v.n, "n is not the model's");
+    if (int rc = check_ids(users, stride, count))
+        return rc;
+    REQUIRE(act >= MFSGD_ACT_NONE && act <= MFSGD_ACT_GELU, "unknown act");
+    REQUIRE(aligned(bias, elem_bytes(dtype)), "bias is misaligned");
+    REQUIRE(matrix_ok(out, count, n, ld_out, dtype), "out is NULL or misaligned, or ld_out is below n");
+    const size_t rows = scores_rows_bytes(v, count);
+    if (int rc = check_work(work, bytes, rows + linear_bytes(count, n, v.KP, dtype)))
+        return rc;
+    if (count == 0)
+        return MFSGD_OK;
+    if (int rc = embed_impl(RowsLaunch{P, m, v.KP, v.KP, dtype, users, stride, count, 1.0f, work, v.KP}, stream))
+        return rc;
+    return linear_impl(LinearLaunch{work, v.Q, bias, nullptr, v.KP, v.KP, 0, count, n, v.KP, dtype, act, out, nullptr,
+                                    ld_out, 0, nullptr},
+                       (char*)work + rows, bytes - (int64_t)rows, stream);
+}
+
 // ---- norms ----
 
 constexpr int64_t kMostTensors = 1 << 20;
@@ -254,6 +336,74 @@ int mfsgd_add_rows(int32_t side, const void* dout, int64_t ld_dout, const int32_
         return embed_grad_impl(RowsGradLaunch{dout, ld_dout, ids, ids_stride, count, k, v.dtype, scale, table, rows,
                                               v.KP, 1, nullptr},
                                workspace, workspace_bytes, stream);
+    });
+}
+
+int mfsgd_linear(const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, const void* residual,
+                 int64_t ldr, int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t act, void* y, int64_t ldy,
+                 void* z, int64_t ldz, void* workspace, int64_t workspace_bytes, void* stream)
+{
+    return guarded([&]() -> int {
+        return linear_impl(LinearLaunch{x, w, bias, residual, ldx, ldw, ldr, M, N, K, dtype, act, y, z, ldy, ldz,
+                                        nullptr},
+                           workspace, workspace_bytes, stream);
+    });
+}
+
+int mfsgd_linear_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, int64_t* bytes)
+{
+    return guarded([&]() -> int {
+        REQUIRE(bytes, "NULL bytes");
+        if (int rc = check_product(M, N, K, dtype))
+            return rc;
+        *bytes = (int64_t)linear_bytes(M, N, K, dtype);
+        return MFSGD_OK;
+    });
+}
+
+int mfsgd_linear_grad(const void* dy, int64_t lddy, const void* z, int64_t ldz, const void* x, int64_t ldx,
+                      const void* w, int64_t ldw, int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t act,
+                      void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias, void* workspace,
+                      int64_t workspace_bytes, void* stream)
+{
+    return guarded([&]() -> int {
+        return linear_grad_impl(LinearGradLaunch{dy, z, x, w, lddy, ldz, ldx, ldw, M, N, K, dtype, act, dx, dw, dbias,
+                                                 lddx, lddw, nullptr},
+                                workspace, workspace_bytes, stream);
+    });
+}
+
+int mfsgd_linear_grad_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, int64_t* bytes)
+{
+    return guarded([&]() -> int {
+        REQUIRE(bytes, "NULL bytes");
+        if (int rc = check_product(M, N, K, dtype))
+            return rc;
+        *bytes = (int64_t)linear_grad_bytes(M, N, K, dtype);
+        return MFSGD_OK;
+    });
+}
+
+int mfsgd_scores(const int32_t* users, int64_t users_stride, int64_t count, int64_t n, int32_t dtype,
+                 const void* bias, int32_t act, void* out, int64_t ld_out, void* workspace, int64_t workspace_bytes,
+                 void* stream)
+{
+    return guarded([&]() -> int {
+        return scores_impl(users, users_stride, count, n, dtype, bias, act, out, ld_out, workspace, workspace_bytes,
+                           stream);
+    });
+}
+
+int mfsgd_scores_workspace(int64_t count, int64_t* bytes)
+{
+    return guarded([&]() -> int {
+        ModelView v;
+        REQUIRE(bytes, "NULL bytes");
+        REQUIRE(count >= 0 && count <= INT32_MAX, "count must be in [0, 2^31-1]");
+        if (!model_view(&v))
+            return set_error(MFSGD_ESTATE, "mfsgd_init has not been called");
+        *bytes = (int64_t)(scores_rows_bytes(v, count) + linear_bytes(count, v.n, v.KP, v.dtype));
+        return MFSGD_OK;
     });
 }
 

@@ -45,6 +45,29 @@ struct RowsGradLaunch {
 size_t rows_grad_bytes(int64_t count, int k);
 hipError_t rows_grad(const RowsGradLaunch& a, hipStream_t st);
 
+// ---- products (ops_linear.hip) ----
+struct LinearLaunch {
+    const void *x, *w, *bias, *residual;
+    int64_t ldx, ldw, ldr, M, N, K;
+    int dtype, act;
+    void *y, *z;
+    int64_t ldy, ldz;
+    void* work;
+};
+size_t linear_bytes(int64_t M, int64_t N, int64_t K, int dtype);
+hipError_t linear(const LinearLaunch& a, hipStream_t st);
+
+struct LinearGradLaunch {
+    const void *dy, *z, *x, *w;
+    int64_t lddy, ldz, ldx, ldw, M, N, K;
+    int dtype, act;
+    void *dx, *dw, *dbias;
+    int64_t lddx, lddw;
+    void* work;
+};
+size_t linear_grad_bytes(int64_t M, int64_t N, int64_t K, int dtype);
+hipError_t linear_grad(const LinearGradLaunch& a, hipStream_t st);
+
 // ---- norms over many tensors (ops_norm.hip) ----
 struct NormTensor {
     void* p; // updated tensor (clip: the gradient itself); nullptr for a norm alone

@@ -26,6 +26,7 @@ OK, EINVAL, ENOMEM, EHIP, ESTATE, ETIMEOUT, ENUMERIC = 0, -1, -2, -3, -4, -5, -6
 BATCH_HOGWILD, WAVEFRONT, WAVEFRONT_DET, GLOBAL_TABLE = 0, 1, 2, 3
 FP32, FP16, BF16 = 0, 1, 2  # BF16: the operators alone
 P, Q = 0, 1
+ACTS = {"none": 0, "relu": 1, "sigmoid": 2, "silu": 3, "gelu": 4}
 DBG_VISITS, DBG_TRACE, DBG_PLAN_STARTS, DBG_PLAN_ORDER, DBG_TEAM_MAP, DBG_TEAM_SIZES = 1, 2, 3, 4, 5, 6
 DBG_TABLE_STARTS, DBG_TABLE_ORDER, DBG_PRIORITY = 7, 8, 9
 
@@ -79,6 +80,14 @@ def lib():
             "mfsgd_embed_grad_workspace": ([i64, i32, C.POINTER(i64)], C.c_int),
             "mfsgd_rows": ([i32, vp, i64, i64, i32, i32, f32, vp, i64, vp], C.c_int),
             "mfsgd_add_rows": ([i32, vp, i64, vp, i64, i64, i32, i32, f32, vp, i64, vp], C.c_int),
+            "mfsgd_linear": ([vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp],
+                             C.c_int),
+            "mfsgd_linear_workspace": ([i64, i64, i64, i32, C.POINTER(i64)], C.c_int),
+            "mfsgd_linear_grad": ([vp, i64, vp, i64, vp, i64, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp,
+                                   vp, i64, vp], C.c_int),
+            "mfsgd_linear_grad_workspace": ([i64, i64, i64, i32, C.POINTER(i64)], C.c_int),
+            "mfsgd_scores": ([vp, i64, i64, i64, i32, vp, i32, vp, i64, vp, i64, vp], C.c_int),
+            "mfsgd_scores_workspace": ([i64, C.POINTER(i64)], C.c_int),
             "mfsgd_grad_norm": ([vp, i64, vp, vp, i64, vp], C.c_int),
             "mfsgd_clip_grads": ([vp, i64, C.c_double, vp, vp, i64, vp], C.c_int),
             "mfsgd_sgd_step": ([vp, vp, i64, f32, f32, C.c_double, vp, vp, i64, vp], C.c_int),
@@ -427,6 +436,94 @@ def add_rows(side: int, dout: torch.Tensor, ids: torch.Tensor, scale: float, str
     work, nbytes, keep = _grad_workspace(on, count, k)
     _check(lib().mfsgd_add_rows(side, dout.data_ptr(), ld, idp, stride, count, k, _DTYPES[dout.dtype], scale, work,
                                 nbytes, on.handle), "mfsgd_add_rows")
+
+
+def _vector(t, what, n, device, dtype):
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.get_device() != device:
+        raise TypeError(f"{what} must be a {dtype} vector on the current GPU")
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what} must be {n} contiguous values")
+    return t.data_ptr()
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, bias=None, residual=None, act: str = "none", out=None,
+           keep_z: bool = False, stream=None):
+    """act(x w^T + bias) + residual for x (M, K) and w (N, K).  With `keep_z`
+    also the pre-activation, which ``linear_grad`` takes: (y, z).  `residual`
+    may be `out` itself."""
+    on = _On(stream)
+    dt = x.dtype if isinstance(x, torch.Tensor) else None
+    ldx, ldw = _matrix(x, "x", on.device), _matrix(w, "w", on.device, dt)
+    (M, K), (N, Kw) = x.shape, w.shape
+    if K != Kw:
+        raise ValueError(f"x has {K} columns, w {Kw}")
+    bp = None if bias is None else _vector(bias, "bias", N, on.device, dt)
+    ldr = 0 if residual is None else _matrix(residual, "residual", on.device, dt, (M, N))
+    if out is None:
+        out = on.empty((M, N), dt)
+        ldy = max(N, 1)
+    else:
+        ldy = _matrix(out, "out", on.device, dt, (M, N))
+    z = on.empty((M, N), dt) if keep_z else None
+    code = _DTYPES[dt]
+    n = C.c_int64()
+    _check(lib().mfsgd_linear_workspace(M, N, K, code, C.byref(n)), "mfsgd_linear_workspace")
+    work, nbytes, keep = on.workspace(n.value)
+    _check(lib().mfsgd_linear(x.data_ptr(), ldx, w.data_ptr(), ldw, bp,
+                              None if residual is None else residual.data_ptr(), ldr, M, N, K, code, ACTS[act],
+                              out.data_ptr(), ldy, z.data_ptr() if keep_z else None, max(N, 1), work, nbytes,
+                              on.handle), "mfsgd_linear")
+    return (out, z) if keep_z else out
+
+
+def linear_grad(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, z=None, act: str = "none", dx: bool = True,
+                dw: bool = True, dbias: bool = True, stream=None):
+    """(dx, dw, dbias) of ``linear`` for dy, the gradient of its result, and the
+    z it kept (not needed without an activation); None for those not asked for.
+    The residual's gradient is dy."""
+    on = _On(stream)
+    dt = x.dtype if isinstance(x, torch.Tensor) else None
+    ldx, ldw = _matrix(x, "x", on.device), _matrix(w, "w", on.device, dt)
+    (M, K), (N, Kw) = x.shape, w.shape
+    if K != Kw:
+        raise ValueError(f"x has {K} columns, w {Kw}")
+    lddy = _matrix(dy, "dy", on.device, dt, (M, N))
+    if z is None and act != "none":
+        raise ValueError("the gradient of an activation needs z")
+    ldz = 0 if z is None else _matrix(z, "z", on.device, dt, (M, N))
+    code = _DTYPES[dt]
+    n = C.c_int64()
+    _check(lib().mfsgd_linear_grad_workspace(M, N, K, code, C.byref(n)), "mfsgd_linear_grad_workspace")
+    work, nbytes, keep = on.workspace(n.value)
+    gx = on.empty((M, K), dt) if dx else None
+    gw = on.empty((N, K), dt) if dw else None
+    gb = on.empty((N,), dt) if dbias else None
+    _check(lib().mfsgd_linear_grad(dy.data_ptr(), lddy, None if z is None else z.data_ptr(), ldz, x.data_ptr(), ldx,
+                                   w.data_ptr(), ldw, M, N, K, code, ACTS[act], gx.data_ptr() if dx else None,
+                                   max(K, 1), gw.data_ptr() if dw else None, max(K, 1),
+                                   gb.data_ptr() if dbias else None, work, nbytes, on.handle), "mfsgd_linear_grad")
+    return gx, gw, gb
+
+
+def scores(users: torch.Tensor, n: int, dtype=None, bias=None, act: str = "none", out=None,
+           stream=None) -> torch.Tensor:
+    """The model's scores of `users` against all its n items:
+    act(p_user . q_item + bias of the item).  A user outside the model: act(bias)."""
+    on = _On(stream)
+    up, stride, count = _ids(users, on.device)
+    dtype = dtype or _storage_dtype()
+    bp = None if bias is None else _vector(bias, "bias", n, on.device, dtype)
+    if out is None:
+        out = on.empty((count, n), dtype)
+        ld = max(n, 1)
+    else:
+        ld = _matrix(out, "out", on.device, dtype, (count, n))
+    need = C.c_int64()
+    _check(lib().mfsgd_scores_workspace(count, C.byref(need)), "mfsgd_scores_workspace")
+    work, nbytes, keep = on.workspace(need.value)
+    _check(lib().mfsgd_scores(up, stride, count, n, _DTYPES[dtype], bp, ACTS[act], out.data_ptr(), ld, work, nbytes,
+                              on.handle), "mfsgd_scores")
+    return out
 
 
 class TensorList:

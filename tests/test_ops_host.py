@@ -146,3 +146,47 @@ def test_norm_workspace(lib):
     for count in (-1, (1 << 20) + 1):
         refused(lib, "mfsgd_norm_workspace", (count, C.byref(n)))
     refused(lib, "mfsgd_norm_workspace", (1, None))
+
+
+LINEAR = dict(x=A, ldx=8, w=A, ldw=8, bias=None, residual=None, ldr=6, M=4, N=6, K=8, dtype=0, act=0, y=A, ldy=6,
+              z=None, ldz=0, work=None, nbytes=0, stream=None)
+LGRAD = dict(dy=A, lddy=6, z=A, ldz=6, x=A, ldx=8, w=A, ldw=8, M=4, N=6, K=8, dtype=0, act=4, dx=A, lddx=8, dw=A,
+             lddw=8, dbias=A, work=A, nbytes=BIG, stream=None)
+
+
+@pytest.mark.parametrize("what", [
+    dict(x=None), dict(x=A + 1), dict(ldx=7), dict(w=None), dict(ldw=7), dict(bias=A + 2), dict(residual=A + 1),
+    dict(residual=A, ldr=5), dict(M=-1), dict(N=-1), dict(K=-1), dict(M=2**31), dict(N=2**31), dict(K=2**31, ldx=2**31),
+    dict(dtype=3), dict(act=5), dict(act=-1), dict(y=None), dict(ldy=5), dict(z=A, ldz=5), dict(z=A + 2, ldz=6),
+    dict(M=64, N=64, K=65536, ldx=65536, ldw=65536, ldy=64), dict(ldx=BIG)])
+def test_linear_refuses(lib, what):
+    refused(lib, "mfsgd_linear", changed(LINEAR, **what))
+
+
+@pytest.mark.parametrize("what", [
+    dict(dy=None), dict(dy=A + 1), dict(lddy=5), dict(z=None), dict(ldz=5), dict(x=None), dict(ldx=7), dict(w=None),
+    dict(ldw=7), dict(M=-1), dict(N=2**31), dict(K=-1), dict(dtype=7), dict(act=9), dict(dx=A + 2), dict(lddx=7),
+    dict(dw=A + 2), dict(lddw=7), dict(dbias=A + 2), dict(work=None), dict(work=A + 64), dict(nbytes=16),
+    dict(nbytes=-1)])
+def test_linear_grad_refuses(lib, what):
+    refused(lib, "mfsgd_linear_grad", changed(LGRAD, **what))
+
+
+def test_product_workspaces(lib):
+    n = C.c_int64(-1)
+    assert lib.mfsgd_linear_workspace(1, 17770, 128, 1, C.byref(n)) == 0 and n.value == 0
+    assert lib.mfsgd_linear_workspace(64, 64, 65536, 0, C.byref(n)) == 0 and n.value > 0
+    for sizes in ((0, 0, 0), (40, 0, 7), (0, 40, 7), (40, 40, 0), (40, 0, 0), (INT32_MAX, 1, 1), (1, INT32_MAX, 1)):
+        for fn in (lib.mfsgd_linear_workspace, lib.mfsgd_linear_grad_workspace):
+            assert fn(*sizes, 0, C.byref(n)) == 0 and n.value >= 0
+    assert lib.mfsgd_linear_grad_workspace(100, 100, 100, 2, C.byref(n)) == 0 and n.value >= 4 * 20_000
+    for fn in ("mfsgd_linear_workspace", "mfsgd_linear_grad_workspace"):
+        for bad in ((-1, 1, 1, 0), (1, 2**31, 1, 0), (1, 1, -5, 0), (1, 1, 1, 3)):
+            refused(lib, fn, (*bad, C.byref(n)))
+        refused(lib, fn, (1, 1, 1, 0, None))
+
+
+def test_scores_need_a_model(lib):
+    n = C.c_int64(-1)
+    refused(lib, "mfsgd_scores_workspace", (5, C.byref(n)), ESTATE)
+    refused(lib, "mfsgd_scores", (A, 1, 4, 100, 0, None, 0, A, 100, A, BIG, None), ESTATE)
