@@ -96,6 +96,10 @@ hipError_t get_typed(const RowsLaunch& a, hipStream_t st)
     return get_launch<T, 1>(a, st);
 }
 
+// A value that every lane of the wavefront has, for the scalar unit: addresses
+// and conditions made of it cost no vector registers and no masks.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // -------------------------------------------------------------- gradient
 //
 // The tokens of one row are added in their order, in binary32, by one of two
@@ -166,10 +170,13 @@ __global__ __launch_bounds__(kThreads) void k_rows_zero(T* __restrict__ out, int
 }
 
 // Few tokens: every id is compared with every other in LDS, one launch and no
-// sort.  A workgroup takes one token at a time; if no earlier token has its id
-// it adds the rows of all that do, each wavefront those of a consecutive part
-// of the tokens, the four sums joined in order.
-constexpr int kScanMost = 4096;
+// sort.  A wavefront takes one token; if no earlier one has its id it adds the
+// rows of all that do.  Where these are more than kScanAlone the workgroup's
+// four wavefronts add a consecutive part of the tokens each, and the four sums
+// are joined in order.
+constexpr int kScanMost = 8192;
+constexpr int kScanAlone = 64;
+constexpr int kScanBlock = 256; // ids compared at a time: four a lane
 
 template <typename T, int E>
 __global__ __launch_bounds__(kThreads) void k_grad_scan(const T* __restrict__ dout, int64_t ld_dout,
@@ -177,62 +184,116 @@ __global__ __launch_bounds__(kThreads) void k_grad_scan(const T* __restrict__ do
                                                         int k, float scale, T* __restrict__ dtable, int64_t rows,
                                                         int64_t ld, int accumulate)
 {
-    __shared__ int32_t all[kScanMost];
+    constexpr int ahead = (int)sizeof(T) * E >= 16 ? 8 : (int)sizeof(T) * E >= 4 ? 16 : 32; // rows in flight
+    __shared__ __attribute__((aligned(16))) int32_t all[kScanMost];
     __shared__ float part[3][64 * E];
-    __shared__ int seen[2][4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ uint16_t list[4][kScanAlone + kScanBlock];
+    __shared__ int more[4]; // the wavefronts' tokens with many rows, or -1
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const Cols c = my_cols<E>(k);
-    for (int j = threadIdx.x; j < count; j += kThreads) {
-        const int32_t id = ids[j * ids_stride];
-        all[j] = id >= 0 && id < rows ? id : -1;
+    const int blocks = (count + kScanBlock - 1) / kScanBlock;
+    for (int j0 = threadIdx.x; j0 < blocks * kScanBlock; j0 += kThreads * 8) {
+        int32_t id[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            id[u] = ids[(j0 + u * kThreads < count ? j0 + u * kThreads : count - 1) * ids_stride];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int j = j0 + u * kThreads;
+            if (j < blocks * kScanBlock)
+                all[j] = j < count && id[u] >= 0 && id[u] < rows ? id[u] : -1;
+        }
     }
     __syncthreads();
-    const int blocks = (count + 63) / 64;
-    int turn = 0;
-    for (int i = blockIdx.x; i < count; i += gridDim.x) {
-        const int32_t r = all[i];
-        if (r < 0)
-            continue;
-        int before = 0;
-        for (int b = wave; b * 64 < i && !before; b += 4) {
-            const int j = b * 64 + lane;
-            before = __ballot(j < i && all[j] == r) != 0;
+
+    float sum[E];
+    // appends the tokens with id r of block b to this wavefront's list of n, in order
+    auto look = [&](int32_t r, int b, int& n) {
+        const int4 id = *(const int4*)&all[b * kScanBlock + lane * 4];
+        const bool is[4] = {id.x == r, id.y == r, id.z == r, id.w == r};
+        if (!__ballot(is[0] || is[1] || is[2] || is[3]))
+            return;
+        int at = n;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint64_t mask = __ballot(is[q]);
+            at += __popcll(mask & ((uint64_t(1) << lane) - 1));
+            n += __popcll(mask);
         }
-        if (lane == 0)
-            seen[turn][wave] = before;
-        __syncthreads();
-        const bool first = !(seen[turn][0] | seen[turn][1] | seen[turn][2] | seen[turn][3]);
-        turn ^= 1; // the other half is free: everyone passed the last barrier after reading it
-        if (!first)
-            continue;
-        float sum[E];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (is[q])
+                list[wave][at++] = (uint16_t)(b * kScanBlock + lane * 4 + q);
+    };
+    // adds the rows of the listed tokens
+    auto add = [&](int n) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+        for (int i0 = 0; i0 < n; i0 += ahead) {
+            Vec<T, E> x[ahead];
+#pragma unroll
+            for (int u = 0; u < ahead; ++u) {
+                const int token = uniform(list[wave][i0 + u < n ? i0 + u : n - 1]);
+                x[u] = load_vec<T, E>(dout + (int64_t)token * ld_dout + c.at);
+            }
+#pragma unroll
+            for (int u = 0; u < ahead; ++u)
+                if (i0 + u < n) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        sum[e] += (float)x[u].v[e];
+                }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    };
+    auto clear = [&] {
 #pragma unroll
         for (int e = 0; e < E; ++e)
             sum[e] = 0.0f;
-        const int b0 = i / 64, each = (blocks - b0 + 3) / 4;
-        const int b1 = b0 + wave * each, b2 = b1 + each < blocks ? b1 + each : blocks;
-        for (int b = b1; b < b2; ++b) {
-            const int j = b * 64 + lane;
-            uint64_t mine = __ballot(j >= i && j < count && all[j < count ? j : 0] == r);
-            while (mine) {
-                int at[4], n = 0;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    at[u] = mine ? __builtin_ctzll(mine) : at[0];
-                    n += mine != 0;
-                    mine &= mine - 1;
-                }
-                Vec<T, E> x[4];
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    x[u] = load_vec<T, E>(dout + (int64_t)(b * 64 + at[u]) * ld_dout + c.at);
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    if (u < n) {
-#pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            sum[e] += (float)x[u].v[e];
-                    }
+    };
+
+    const int i = (int)blockIdx.x * 4 + wave, home = i / kScanBlock;
+    const int32_t r = i < count ? uniform(all[i]) : -1;
+    int many = -1;
+    if (r >= 0) {
+        bool earlier = false;
+        for (int b = 0; b < home && !earlier; ++b) {
+            const int4 id = *(const int4*)&all[b * kScanBlock + lane * 4];
+            earlier = __ballot(id.x == r || id.y == r || id.z == r || id.w == r) != 0;
+        }
+        int n = 0;
+        if (!earlier) {
+            look(r, home, n);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+            earlier = uniform(list[wave][0]) < i; // the first in its block
+        }
+        if (!earlier) {
+            for (int b = home + 1; b < blocks && n <= kScanAlone; ++b)
+                look(r, b, n);
+            if (n > kScanAlone) {
+                many = i;
+            } else {
+                clear();
+                add(n);
+                write_row<T, E>(dtable + (int64_t)r * ld, c, sum, scale, accumulate);
+            }
+        }
+    }
+    if (lane == 0)
+        more[wave] = many;
+    __syncthreads();
+    for (int w = 0; w < 4; ++w) {
+        const int first = uniform(more[w]);
+        if (first < 0)
+            continue;
+        const int32_t id = uniform(all[first]);
+        const int b0 = first / kScanBlock, each = (blocks - b0 + 3) / 4, from = b0 + wave * each;
+        const int to = from + each < blocks ? from + each : blocks;
+        clear();
+        for (int b = from, n = 0; b < to; ++b) {
+            look(id, b, n);
+            if (n >= kScanAlone || b + 1 == to) {
+                add(n);
+                n = 0;
             }
         }
         if (wave) {
@@ -243,11 +304,11 @@ __global__ __launch_bounds__(kThreads) void k_grad_scan(const T* __restrict__ do
         __syncthreads();
         if (wave == 0) {
 #pragma unroll
-            for (int w = 0; w < 3; ++w)
+            for (int v = 0; v < 3; ++v)
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    sum[e] += part[w][e * 64 + lane];
-            write_row<T, E>(dtable + (int64_t)r * ld, c, sum, scale, accumulate);
+                    sum[e] += part[v][e * 64 + lane];
+            write_row<T, E>(dtable + (int64_t)id * ld, c, sum, scale, accumulate);
         }
         __syncthreads();
     }
@@ -256,11 +317,10 @@ __global__ __launch_bounds__(kThreads) void k_grad_scan(const T* __restrict__ do
 // Many tokens: (row, token) pairs sorted by row, stably, so that a row's tokens
 // stay in order; then tiles of the sorted tokens summed by one wavefront each.
 //
-// The sort is by digits of `bits` bits from the lowest: per chunk of kChunk
+// The sort is by digits of `bits` bits from the lowest: per chunk of
 // tokens the count of every digit, the exclusive sums of these over the chunks,
 // and every token to its place.  Tokens without a row have the key `rows` and
 // end up last.
-constexpr int kChunk = 4096;
 constexpr int kDigits = 256;
 
 __device__ __forceinline__ uint32_t key_of(int32_t id, int64_t rows)
@@ -268,6 +328,7 @@ __device__ __forceinline__ uint32_t key_of(int32_t id, int64_t rows)
     return id >= 0 && id < rows ? (uint32_t)id : (uint32_t)rows;
 }
 
+template <int CHUNK>
 __global__ __launch_bounds__(kThreads) void k_sort_count(const uint32_t* __restrict__ keys,
                                                          const int32_t* __restrict__ ids, int64_t ids_stride,
                                                          int64_t rows, int64_t count, int shift, uint32_t mask,
@@ -276,13 +337,15 @@ __global__ __launch_bounds__(kThreads) void k_sort_count(const uint32_t* __restr
     __shared__ uint32_t n[kDigits];
     n[threadIdx.x] = 0;
     __syncthreads();
-    const int64_t base = (int64_t)blockIdx.x * kChunk;
-#pragma unroll 4
-    for (int j = threadIdx.x; j < kChunk; j += kThreads)
+    const int64_t base = (int64_t)blockIdx.x * CHUNK;
+#pragma unroll
+    for (int s = 0; s < CHUNK / kThreads; ++s) {
+        const int j = s * kThreads + (int)threadIdx.x;
         if (base + j < count) {
             const uint32_t key = keys ? keys[base + j] : key_of(ids[(base + j) * ids_stride], rows);
             atomicAdd(&n[key >> shift & mask], 1u);
         }
+    }
     __syncthreads();
     if (threadIdx.x <= mask)
         hist[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] = n[threadIdx.x];
@@ -293,7 +356,7 @@ __global__ __launch_bounds__(kThreads) void k_sort_count(const uint32_t* __restr
 // Exclusive sum of x over the workgroup's 256 threads; `total` is its sum.
 __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t* wave_sums, uint32_t& total)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     uint32_t s = x;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -333,6 +396,7 @@ __global__ __launch_bounds__(kThreads) void k_sort_scan(uint32_t* __restrict__ h
         totals[blockIdx.x] = carry;
 }
 
+template <int CHUNK>
 __global__ __launch_bounds__(kThreads) void k_sort_place(const uint32_t* __restrict__ keys,
                                                          const uint32_t* __restrict__ toks,
                                                          const int32_t* __restrict__ ids, int64_t ids_stride,
@@ -342,12 +406,12 @@ __global__ __launch_bounds__(kThreads) void k_sort_place(const uint32_t* __restr
                                                          uint32_t* __restrict__ keys_out,
                                                          uint32_t* __restrict__ toks_out)
 {
-    constexpr int steps = kChunk / kThreads; // 64 consecutive tokens a step, a wavefront's steps consecutive
+    constexpr int steps = CHUNK / kThreads; // 64 consecutive tokens a step, a wavefront's steps consecutive
     __shared__ uint32_t next[4][kDigits];
     __shared__ uint32_t sums[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const uint32_t mask = (1u << bits) - 1;
-    const int64_t base = (int64_t)blockIdx.x * kChunk + wave * (steps * 64) + lane;
+    const int64_t base = (int64_t)blockIdx.x * CHUNK + wave * (steps * 64) + lane;
 #pragma unroll
     for (int w = 0; w < 4; ++w)
         next[w][threadIdx.x] = 0;
@@ -401,12 +465,12 @@ __global__ __launch_bounds__(kThreads) void k_sort_place(const uint32_t* __restr
 }
 
 // The sums over the sorted tokens.  A wavefront adds the rows of one tile of
-// `tile` tokens, kBatch loads in flight.  A row whose tokens lie inside one tile
-// is written at once.  Of one that goes on, the tile where it begins keeps its
-// sum in `tails` and notes the tile in `begun`, every later tile its own in
-// `heads`; k_grad_join adds those up in order.  The workgroups past the tiles
-// write zeros to the rows that no token has.
-constexpr int kBatch = 8;
+// `tile` tokens, several loads in flight.  A row whose tokens end in the tile
+// they begin in, or in the next one, is added up and written by the tile where
+// it begins.  Of a longer one that tile keeps its sum in `tails` and notes
+// itself and the number of tiles in `begun`, every later tile its own in
+// `heads`; k_grad_join adds those up in order.  The workgroups before the tiles write zeros to the rows that no
+// token has (first, because they take longest from their start to their end).
 
 // Zeros in those of `here` rows whose bit of `taken` is clear, by one wavefront.
 template <typename T, int V>
@@ -425,111 +489,208 @@ __device__ __forceinline__ void zero_rows(T* __restrict__ out, int64_t ld, int k
     }
 }
 
-template <typename T, int E>
+// The first of the sorted keys that is not below `key` (count: none), found by
+// a wavefront 64 places at a time.
+__device__ __forceinline__ int64_t first_at_least(const uint32_t* __restrict__ keys, int64_t count, uint32_t key,
+                                                  int lane)
+{
+    int64_t lo = 0, hi = count; // keys before lo are below it, keys from hi on are not
+    while (hi > lo) {
+        const int64_t step = (hi - lo + 63) / 64, p = lo + (lane + 1) * step - 1;
+        const uint64_t not_below = __ballot(p >= hi || keys[p < hi ? p : lo] >= key);
+        const int f = not_below ? __builtin_ctzll(not_below) : 64;
+        const int64_t next = lo + f * step;
+        hi = f < 64 && next + step - 1 < hi ? next + step - 1 : hi;
+        lo = next < hi ? next : hi;
+    }
+    return lo;
+}
+
+// The sum of a row to its place, added to what was read from there if ACC.
+template <typename T, int E, bool ACC>
+__device__ __forceinline__ void put_row(T* row, const Cols& c, const float (&sum)[E], float scale, const Vec<T, E>& old)
+{
+    Vec<T, E> x;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        x.v[e] = ACC ? T((float)old.v[e] + scale * sum[e]) : T(scale * sum[e]);
+    if (ACC && c.skip) { // a shared element is the other lane's to add to
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (e >= c.skip)
+                row[c.at + e] = x.v[e];
+    } else if (c.skip < E) {
+        store_vec<T, E>(row + c.at, x);
+    }
+}
+
+template <typename T, int E, bool ACC>
 __global__ __launch_bounds__(kThreads) void k_grad_tiles(const T* __restrict__ dout, int64_t ld_dout,
                                                          const uint32_t* __restrict__ keys,
                                                          const uint32_t* __restrict__ toks, int64_t count, int k,
                                                          float scale, T* __restrict__ dtable, int64_t rows, int64_t ld,
-                                                         int accumulate, int tile, int64_t tiles, int tile_wgs,
+                                                         int tile, int64_t tiles, int zero_wgs,
                                                          float* __restrict__ heads, float* __restrict__ tails,
-                                                         uint32_t* __restrict__ begun, uint32_t* __restrict__ crossing,
-                                                         FastDiv nv)
+                                                         uint2* __restrict__ begun, uint32_t* __restrict__ crossing,
+                                                         FastDiv per_row)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if ((int)blockIdx.x >= tile_wgs) {
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    if ((int)blockIdx.x < zero_wgs) {
         if (blockIdx.y)
             return;
-        const int64_t stride = (int64_t)(gridDim.x - tile_wgs) * 256;
-        for (int64_t r0 = ((int64_t)(blockIdx.x - tile_wgs) * 4 + wave) * 64; r0 < rows; r0 += stride) {
-            const uint32_t r = (uint32_t)(r0 + lane < rows ? r0 + lane : rows - 1);
-            int64_t lo = 0, hi = count; // first sorted token whose key is not below r
-            while (lo < hi) {
-                const int64_t mid = (lo + hi) >> 1;
-                if (keys[mid] < r)
-                    lo = mid + 1;
-                else
-                    hi = mid;
+        const int64_t stride = (int64_t)zero_wgs * 256;
+        for (int64_t r0 = ((int64_t)blockIdx.x * 4 + wave) * 64; r0 < rows; r0 += stride) {
+            // the tokens of these 64 rows, then a bit for every row that has one
+            int64_t lo = first_at_least(keys, count, (uint32_t)r0, lane);
+            const int64_t hi = first_at_least(keys, count, (uint32_t)(r0 + 64 < rows ? r0 + 64 : rows), lane);
+            uint64_t taken = 0;
+            if (hi - lo <= 1024) {
+#pragma unroll 4
+                for (; lo < hi; lo += 64)
+                    taken |= uint64_t(lo + lane < hi) << (keys[lo + lane < hi ? lo + lane : lo] - (uint32_t)r0);
+#pragma unroll
+                for (int d = 32; d > 0; d >>= 1)
+                    taken |= __shfl_xor((unsigned long long)taken, d, 64);
+            } else {
+                const uint32_t r = (uint32_t)r0 + lane;
+                int64_t p = lo, q = hi; // first of them whose key is not below r
+                while (p < q) {
+                    const int64_t mid = (p + q) >> 1;
+                    if (keys[mid] < r)
+                        p = mid + 1;
+                    else
+                        q = mid;
+                }
+                taken = __ballot(p < hi && keys[p < hi ? p : lo] == r);
             }
-            const uint64_t taken = __ballot(lo < count && keys[lo < count ? lo : 0] == r);
             const int here = (int)(rows - r0 < 64 ? rows - r0 : 64);
             constexpr int most = 16 / (int)sizeof(T);
             if (k >= most)
-                zero_rows<T, most>(dtable + r0 * ld, ld, k, here, taken, nv);
+                zero_rows<T, most>(dtable + r0 * ld, ld, k, here, taken, per_row);
             else if (k >= most / 2)
-                zero_rows<T, most / 2>(dtable + r0 * ld, ld, k, here, taken, nv);
+                zero_rows<T, most / 2>(dtable + r0 * ld, ld, k, here, taken, per_row);
             else if (most == 8 && k >= 2)
-                zero_rows<T, 2>(dtable + r0 * ld, ld, k, here, taken, nv);
+                zero_rows<T, 2>(dtable + r0 * ld, ld, k, here, taken, per_row);
             else
-                zero_rows<T, 1>(dtable + r0 * ld, ld, k, here, taken, nv);
+                zero_rows<T, 1>(dtable + r0 * ld, ld, k, here, taken, per_row);
         }
         return;
     }
-    const int64_t t = (int64_t)blockIdx.x * 4 + wave;
+    const int64_t t = (int64_t)(blockIdx.x - zero_wgs) * 4 + wave;
     if (t >= tiles)
         return;
+    constexpr int batch = ACC || (int)sizeof(T) * E >= 16 ? 8 : 16;
     const Cols c = my_cols<E>(k);
     const int64_t start = t * tile;
     const int n = (int)(count - start < tile ? count - start : tile);
-    const uint32_t none = 0xffffffffu, out_of_rows = (uint32_t)rows;
-    const uint32_t key = keys[start + (lane < n ? lane : n - 1)], tok = toks[start + (lane < n ? lane : n - 1)];
-    const uint32_t prev = start > 0 ? keys[start - 1] : none, after = start + n < count ? keys[start + n] : none;
-    uint32_t cur = __builtin_amdgcn_readfirstlane(key);
-    if (cur == out_of_rows)
+    const uint32_t none = 0xffffffffu;
+    uint32_t key = keys[start + (lane < n ? lane : n - 1)], tok = toks[start + (lane < n ? lane : n - 1)];
+    // the keys before the tile and behind it, before the previous tile and behind the next one
+    const uint32_t prev = start > 0 ? keys[start - 1] : none;
+    const uint32_t next = start + n < count ? keys[start + n] : none;
+    const uint32_t before = start > tile ? keys[start - tile - 1] : none;
+    const uint32_t beyond = start + 2 * tile < count ? keys[start + 2 * tile] : none;
+    const int nv = __popcll(__ballot(lane < n && key < (uint32_t)rows)); // tokens with a row come first
+    if (nv == 0)
         return;
-    bool head = prev == cur;
+    const uint32_t after = nv < n ? none : next;
+    const uint32_t first = __builtin_amdgcn_readlane(key, 0), last = __builtin_amdgcn_readlane(key, nv - 1);
+    // a bit for every token that begins a row, and one for every token (but the last) that ends one
+    const uint32_t left = (uint32_t)__shfl_up((int)key, 1, 64);
+    const uint64_t starts = __ballot(lane == 0 || key != left) & (~uint64_t(0) >> (64 - nv));
+    const uint64_t ends = starts >> 1;
     float sum[E];
+    // adds tokens [from, to) of those the lanes hold, writing every row that ends before the last token
+    auto add = [&](int from, int to, uint64_t starts, uint64_t ends) {
+        for (; from < to; from += batch) {
+            Vec<T, E> x[batch], old[ACC ? batch : 1];
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-        sum[e] = 0.0f;
-    auto flush = [&](bool tail) {
-        if (!head && !tail) {
-            write_row<T, E>(dtable + (int64_t)cur * ld, c, sum, scale, accumulate);
-            return;
-        }
-        float* to = (head ? heads : tails) + t * k + c.at;
-        if (c.skip < E) {
+            for (int u = 0; u < batch; ++u) {
+                const uint32_t row = __builtin_amdgcn_readlane(tok, from + u < to ? from + u : to - 1);
+                x[u] = load_vec<T, E>(dout + (int64_t)row * ld_dout + c.at);
+            }
+            if (ACC) {
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                to[e] = sum[e];
-        }
-        if (!head && blockIdx.y == 0 && lane == 0)
-            begun[atomicAdd(crossing, 1u)] = (uint32_t)t;
-    };
-    for (int j0 = 0; j0 < n; j0 += kBatch) {
-        Vec<T, E> x[kBatch];
+                for (int u = 0; u < batch; ++u) {
+                    const uint32_t row = __builtin_amdgcn_readlane(key, from + u < to ? from + u : to - 1);
+                    if (ends >> (from + u) & 1)
+                        old[u] = load_vec<T, E>(dtable + (int64_t)row * ld + c.at);
+                }
+            }
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            const uint32_t row = __builtin_amdgcn_readlane(tok, j0 + u < n ? j0 + u : n - 1);
-            x[u] = load_vec<T, E>(dout + (int64_t)row * ld_dout + c.at);
-        }
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            if (j0 + u < n) {
-                const uint32_t at = __builtin_amdgcn_readlane(key, j0 + u);
-                if (at != cur) {
-                    flush(false);
-                    if (at == out_of_rows)
-                        return;
-                    cur = at;
-                    head = false;
+            for (int u = 0; u < batch; ++u) {
+                if (from + u < to) {
+                    const bool fresh = starts >> (from + u) & 1;
 #pragma unroll
                     for (int e = 0; e < E; ++e)
-                        sum[e] = 0.0f;
+                        sum[e] = (fresh ? 0.0f : sum[e]) + (float)x[u].v[e];
+                    if (ends >> (from + u) & 1) {
+                        const uint32_t row = __builtin_amdgcn_readlane(key, from + u);
+                        put_row<T, E, ACC>(dtable + (int64_t)row * ld, c, sum, scale, old[ACC ? u : 0]);
+                    }
                 }
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    sum[e] += (float)x[u].v[e];
             }
         }
+    };
+    auto keep = [&](float* parts) {
+        if (c.skip < E) {
+            float* part = parts + t * k + c.at;
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                part[e] = sum[e];
+        }
+    };
+    int from = 0;
+    if (prev == first) {
+        const uint64_t more = starts & ~uint64_t(1);
+        const int h = more ? __builtin_ctzll(more) : nv; // tokens of the row that began before
+        if (h == nv && after == first) { // all of them, and it goes on
+            add(0, nv, 1, 0);
+            keep(heads);
+            return;
+        }
+        if (before == first) { // the end of a row over several tiles (else the previous tile's, whose last row it is)
+            add(0, h, 1, 0);
+            keep(heads);
+        }
+        from = h;
+        if (from == nv)
+            return;
     }
-    flush(after == cur);
+    add(from, nv, starts, ends);
+    if (after == last) {
+        if (beyond == last) {
+            keep(tails);
+            if (blockIdx.y)
+                return;
+            // the last tile that begins with this key: tile `lo` does, tile `hi` does not; 64 places between them a
+            // step
+            int64_t lo = t + 1, hi = tiles;
+            while (hi - lo > 1) {
+                const int64_t step = (hi - lo + 63) / 64, p = lo + (lane + 1) * step;
+                const int f = __builtin_ctzll(__ballot(p >= hi || keys[(p < hi ? p : lo) * tile] != last));
+                const int64_t top = lo + (f + 1) * step;
+                lo += f * step;
+                hi = top < hi ? top : hi;
+            }
+            if (lane == 0)
+                begun[atomicAdd(crossing, 1u)] = make_uint2((uint32_t)t, (uint32_t)(lo - t) + 1);
+            return;
+        }
+        // it ends in the next tile: its tokens there
+        const int64_t on = start + tile;
+        const int m = (int)(count - on < tile ? count - on : tile);
+        key = keys[on + (lane < m ? lane : m - 1)];
+        tok = toks[on + (lane < m ? lane : m - 1)];
+        add(0, __popcll(__ballot(lane < m && key == last)), 0, 0);
+    }
+    write_row<T, E>(dtable + (int64_t)last * ld, c, sum, scale, ACC);
 }
 
-// Joins the rows that go on over several tiles: tails[a], then heads[a + 1 ..
-// b], where b is the last tile that begins with the row's key.  A wavefront
-// takes one such row a round and adds it alone up to kJoinAlone tiles; a longer
-// one is then added by the whole workgroup, its wavefronts taking consecutive
-// parts that are joined in order.
+// Joins the rows that go on over several tiles: tails[a], then the heads of the
+// tiles after it.  A wavefront takes one such row a round and adds it alone up to
+// kJoinAlone tiles; a longer one is then added by the whole workgroup, its
+// wavefronts taking consecutive parts that are joined in order.
 constexpr int kJoinThreads = 1024;
 constexpr int kJoinAlone = 32;
 
@@ -537,15 +698,16 @@ template <int E>
 __device__ __forceinline__ void add_parts(const float* __restrict__ heads, const float* __restrict__ tails, int64_t a,
                                           int from, int to, int k, const Cols& c, float (&sum)[E])
 {
-    for (int i0 = from; i0 < to; i0 += kBatch) {
-        Vec<float, E> x[kBatch];
+    constexpr int batch = E <= 2 ? 16 : 8;
+    for (int i0 = from; i0 < to; i0 += batch) {
+        Vec<float, E> x[batch];
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
+        for (int u = 0; u < batch; ++u) {
             const int i = i0 + u < to ? i0 + u : to - 1;
             x[u] = load_vec<float, E>((i ? heads : tails) + (a + i) * k + c.at);
         }
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u)
+        for (int u = 0; u < batch; ++u)
             if (i0 + u < to) {
 #pragma unroll
                 for (int e = 0; e < E; ++e)
@@ -557,36 +719,29 @@ __device__ __forceinline__ void add_parts(const float* __restrict__ heads, const
 template <typename T, int E>
 __global__ __launch_bounds__(kJoinThreads) void k_grad_join(const uint32_t* __restrict__ keys, int k, float scale,
                                                             T* __restrict__ dtable, int64_t ld, int accumulate,
-                                                            int tile, int64_t tiles, const float* __restrict__ heads,
+                                                            int tile, const float* __restrict__ heads,
                                                             const float* __restrict__ tails,
-                                                            const uint32_t* __restrict__ begun,
+                                                            const uint2* __restrict__ begun,
                                                             const uint32_t* __restrict__ crossing)
 {
     constexpr int waves = kJoinThreads / 64;
     __shared__ float part[waves][64 * E];
     __shared__ int long_at[waves], long_span[waves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const Cols c = my_cols<E>(k);
     const int64_t n = *crossing;
     float sum[E];
-    for (int64_t i0 = (int64_t)blockIdx.x * waves; i0 < n; i0 += (int64_t)gridDim.x * waves) {
+    // the rows are dealt to the workgroups one at a time, so that a few rows meet many workgroups
+    for (int64_t i0 = blockIdx.x; i0 < n; i0 += (int64_t)gridDim.x * waves) {
         int span = 0;
-        if (i0 + wave < n) {
-            const int64_t a = __builtin_amdgcn_readfirstlane((int)begun[i0 + wave]);
-            const uint32_t key = __builtin_amdgcn_readfirstlane((int)keys[(a + 1) * tile]);
-            // tile `lo` begins with the key, tile `hi` does not; 64 places between them a step
-            int64_t lo = a + 1, hi = tiles;
-            while (hi - lo > 1) {
-                const int64_t step = (hi - lo + 63) / 64, p = lo + (lane + 1) * step;
-                const int f = __builtin_ctzll(__ballot(p >= hi || keys[(p < hi ? p : lo) * tile] != key));
-                const int64_t top = lo + (f + 1) * step;
-                lo += f * step;
-                hi = top < hi ? top : hi;
-            }
-            span = (int)(lo - a) + 1;
+        const int64_t i = i0 + (int64_t)wave * gridDim.x;
+        if (i < n) {
+            const int64_t a = uniform((int)begun[i].x);
+            span = uniform((int)begun[i].y);
             if (lane == 0)
                 long_at[wave] = (int)a;
             if (span <= kJoinAlone) {
+                const uint32_t key = uniform((int)keys[(a + 1) * tile]);
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     sum[e] = 0.0f;
@@ -598,10 +753,10 @@ __global__ __launch_bounds__(kJoinThreads) void k_grad_join(const uint32_t* __re
             long_span[wave] = span;
         __syncthreads();
         for (int w = 0; w < waves; ++w) {
-            const int total = long_span[w];
+            const int total = uniform(long_span[w]);
             if (total <= kJoinAlone)
                 continue;
-            const int64_t a = long_at[w];
+            const int64_t a = uniform(long_at[w]);
             const int each = (total + waves - 1) / waves, from = wave * each;
             const int to = from + each < total ? from + each : total;
 #pragma unroll
@@ -656,10 +811,28 @@ hipError_t zero_typed(const RowsGradLaunch& a, hipStream_t st)
 
 // Tokens of a tile: 64, or fewer where that leaves the chip without enough
 // wavefronts to cover the loads' latency.
-int tile_of(int64_t count) { return count >= 64 * 4096 ? 64 : count >= 32 * 4096 ? 32 : 16; }
+int tile_of(int64_t count) { return count >= 64 * 8192 ? 64 : count >= 32 * 8192 ? 32 : 16; }
+
+// Tokens of a chunk of the sort: as few as still give every CU one (the sort's
+// kernels are bound by their chains of dependent steps), but not so many chunks
+// that their counts outweigh the tokens.
+int chunk_of(int64_t count) { return count <= 1024 * 2048 ? 1024 : 4096; }
+
+template <int CHUNK>
+void sort_pass(const uint32_t* keys, const uint32_t* toks, const RowsGradLaunch& a, int shift, int bits, uint32_t* hist,
+               uint32_t* totals, uint32_t* crossing, uint32_t* keys_out, uint32_t* toks_out, hipStream_t st)
+{
+    const unsigned chunks = (unsigned)((a.count + CHUNK - 1) / CHUNK);
+    hipLaunchKernelGGL(k_sort_count<CHUNK>, dim3(chunks), dim3(kThreads), 0, st, keys, a.ids, a.ids_stride, a.rows,
+                       a.count, shift, (1u << bits) - 1, hist, crossing);
+    hipLaunchKernelGGL(k_sort_scan, dim3(1u << bits), dim3(kThreads), 0, st, hist, (int)chunks, totals);
+    hipLaunchKernelGGL(k_sort_place<CHUNK>, dim3(chunks), dim3(kThreads), 0, st, keys, toks, a.ids, a.ids_stride,
+                       a.rows, a.count, shift, bits, hist, totals, keys_out, toks_out);
+}
 
 struct GradWork {
-    uint32_t *keys[2], *toks[2], *hist, *totals, *crossing, *begun;
+    uint32_t *keys[2], *toks[2], *hist, *totals, *crossing;
+    uint2* begun;
     float *heads, *tails;
     size_t bytes;
 };
@@ -681,7 +854,7 @@ GradWork grad_work(int64_t count, int k, void* base)
         at += round256(bytes);
         return p;
     };
-    const size_t chunks = (size_t)((count + kChunk - 1) / kChunk);
+    const size_t chunks = (size_t)((count + chunk_of(count) - 1) / chunk_of(count));
     const size_t tiles = (size_t)((count + tile_of(count) - 1) / tile_of(count));
     for (int i = 0; i < 2; ++i) {
         w.keys[i] = (uint32_t*)part(4 * (size_t)count);
@@ -690,7 +863,7 @@ GradWork grad_work(int64_t count, int k, void* base)
     w.hist = (uint32_t*)part(4 * chunks * kDigits);
     w.totals = (uint32_t*)part(4 * kDigits);
     w.crossing = (uint32_t*)part(4);
-    w.begun = (uint32_t*)part(4 * tiles);
+    w.begun = (uint2*)part(8 * tiles);
     w.heads = (float*)part(4 * tiles * (size_t)k);
     w.tails = (float*)part(4 * tiles * (size_t)k);
     w.bytes = at;
@@ -709,23 +882,18 @@ hipError_t grad_launch(const RowsGradLaunch& a, hipStream_t st)
         }
         if (a.count == 0)
             return hipSuccess;
-        hipLaunchKernelGGL((k_grad_scan<T, E>), dim3((unsigned)std::min<int64_t>(a.count, 2048), ys), dim3(kThreads), 0,
+        hipLaunchKernelGGL((k_grad_scan<T, E>), dim3((unsigned)((a.count + 3) / 4), ys), dim3(kThreads), 0,
                            st, (const T*)a.dout, a.ld_dout, a.ids, a.ids_stride, (int)a.count, a.k, a.scale,
                            (T*)a.dtable, a.rows, a.ld, a.accumulate);
         return hipGetLastError();
     }
     const GradWork w = grad_work(a.count, a.k, a.work);
-    const unsigned chunks = (unsigned)((a.count + kChunk - 1) / kChunk);
     const int bits = key_bits(a.rows), passes = (bits + 7) / 8, width = (bits + passes - 1) / passes;
     const uint32_t *keys = nullptr, *toks = nullptr;
     for (int p = 0; p < passes; ++p) {
         const int shift = p * width, now = std::min(width, bits - shift);
-        const uint32_t mask = (1u << now) - 1;
-        hipLaunchKernelGGL(k_sort_count, dim3(chunks), dim3(kThreads), 0, st, keys, a.ids, a.ids_stride, a.rows,
-                           a.count, shift, mask, w.hist, w.crossing);
-        hipLaunchKernelGGL(k_sort_scan, dim3(1u << now), dim3(kThreads), 0, st, w.hist, (int)chunks, w.totals);
-        hipLaunchKernelGGL(k_sort_place, dim3(chunks), dim3(kThreads), 0, st, keys, toks, a.ids, a.ids_stride, a.rows,
-                           a.count, shift, now, w.hist, w.totals, w.keys[p & 1], w.toks[p & 1]);
+        (chunk_of(a.count) == 1024 ? sort_pass<1024> : sort_pass<4096>)(keys, toks, a, shift, now, w.hist, w.totals,
+                                                                       w.crossing, w.keys[p & 1], w.toks[p & 1], st);
         keys = w.keys[p & 1];
         toks = w.toks[p & 1];
     }
@@ -734,12 +902,12 @@ hipError_t grad_launch(const RowsGradLaunch& a, hipStream_t st)
     const int tile_wgs = (int)((tiles + 3) / 4);
     const int zero_wgs = a.accumulate ? 0 : (int)std::min<int64_t>((a.rows + 255) / 256, 1 << 20);
     const int v = vec_of<T>(a.k);
-    hipLaunchKernelGGL((k_grad_tiles<T, E>), dim3((unsigned)(tile_wgs + zero_wgs), ys), dim3(kThreads), 0, st,
-                       (const T*)a.dout, a.ld_dout, keys, toks, a.count, a.k, a.scale, (T*)a.dtable, a.rows, a.ld,
-                       a.accumulate, tile, tiles, tile_wgs, w.heads, w.tails, w.begun, w.crossing,
-                       fast_div((uint32_t)((a.k + v - 1) / v)));
+    hipLaunchKernelGGL((a.accumulate ? k_grad_tiles<T, E, true> : k_grad_tiles<T, E, false>),
+                       dim3((unsigned)(tile_wgs + zero_wgs), ys), dim3(kThreads), 0, st, (const T*)a.dout, a.ld_dout,
+                       keys, toks, a.count, a.k, a.scale, (T*)a.dtable, a.rows, a.ld, tile, tiles, zero_wgs, w.heads,
+                       w.tails, w.begun, w.crossing, fast_div((uint32_t)((a.k + v - 1) / v)));
     hipLaunchKernelGGL((k_grad_join<T, E>), dim3((unsigned)std::min<int64_t>((tiles + 15) / 16, 256), ys),
-                       dim3(kJoinThreads), 0, st, keys, a.k, a.scale, (T*)a.dtable, a.ld, a.accumulate, tile, tiles,
+                       dim3(kJoinThreads), 0, st, keys, a.k, a.scale, (T*)a.dtable, a.ld, a.accumulate, tile,
                        w.heads, w.tails, w.begun, w.crossing);
     return hipGetLastError();
 }

@@ -98,8 +98,8 @@ def make_ids(kind, count, rows, g):
 @pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
 @pytest.mark.parametrize("kind", ["uniform", "same", "sorted", "none", "skewed"])
 @pytest.mark.parametrize("count,rows,k", [(1, 1, 1), (5, 7, 3), (64, 300, 33), (65, 2, 128), (1000, 257, 100),
-                                          (4096, 50, 64), (4097, 70_001, 5), (5000, 255, 130), (9_999, 256, 1100),
-                                          (70_000, 1, 2), (70_000, 5000, 257), (140_000, 300, 64)])
+                                          (4096, 50, 64), (8191, 9000, 5), (8192, 50, 64), (8193, 70_001, 5), (9000, 255, 130), (9_999, 256, 1100),
+                                          (70_000, 1, 2), (70_000, 5000, 257), (9_999, 300, 513), (140_000, 300, 64)])
 def test_embed_grad_is_the_exact_sum(dtype, kind, count, rows, k):
     g = rng(count + rows)
     dout, _ = pitched(count, k, k + 1, dtype, shift=1)
@@ -131,6 +131,22 @@ def test_embed_grad_long_rows():
     assert torch.equal(got.double(), grad_want(dout, ids, rows, 1.0))
 
 
+@pytest.mark.parametrize("count", [7_000, 16_000, 280_000, 560_000])
+def test_embed_grad_rows_of_every_length(count):
+    """Rows whose sorted tokens begin and end at, before and after every kind of boundary between the kernels'
+    tiles, one to four tiles long."""
+    lengths = [1, 2, 15, 16, 17, 31, 32, 33, 47, 48, 49, 63, 64, 65, 95, 96, 97, 127, 128, 129, 191, 192, 193, 255, 256, 257]
+    g = rng(count)
+    pick = torch.tensor(lengths, device="cuda")[torch.randint(0, len(lengths), (count,), generator=g, device="cuda")]
+    ids = torch.repeat_interleave(torch.arange(count, device="cuda"), pick)[:count].int()
+    rows = int(ids[-1]) + 2
+    order = torch.randperm(count, generator=g, device="cuda")
+    for t in (ids, ids[order].contiguous(), torch.where(ids % 5 == 0, -1, ids).int()):
+        dout = torch.randint(-4, 5, (count, 3), generator=g, device="cuda").float()
+        got = M.embed_grad(dout, t, rows)
+        assert torch.equal(got.double(), grad_want(dout, t, rows, 1.0))
+
+
 @pytest.mark.parametrize("count", [900, 60_000])
 def test_embed_grad_rounding_and_repeat(count):
     """Random values: n terms added in binary32 are off by at most (n - 1) 2^-24 of the sum of their
@@ -150,7 +166,7 @@ def test_embed_grad_rounding_and_repeat(count):
             assert torch.equal(got, M.embed_grad(dout, ids, rows, scale=0.3))
 
 
-@pytest.mark.parametrize("count", [300, 6000])
+@pytest.mark.parametrize("count", [300, 16_000])
 def test_embed_grad_leaves_padding_out(count):
     """What stands in a padded token's row reaches nothing, NaN and infinity included."""
     g = rng(5)
@@ -197,8 +213,8 @@ def test_offsets_past_32_bits():
 def test_streams_and_graphs():
     """On another stream, and captured: every replay sees the inputs as they are then."""
     g = rng(9)
-    ids = make_ids("skewed", 6000, 500, g)
-    dout = torch.randint(-4, 5, (6000, 40), generator=g, device="cuda").float()
+    ids = make_ids("skewed", 16_000, 500, g)
+    dout = torch.randint(-4, 5, (16_000, 40), generator=g, device="cuda").float()
     table = torch.randint(-4, 5, (500, 40), generator=g, device="cuda").float()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -212,8 +228,8 @@ def test_streams_and_graphs():
         many = M.embed_grad(dout, ids, 500)
         rows = M.embed(table, ids, scale=2.0)
     for step in range(4):
-        ids.copy_(make_ids("skewed" if step % 2 else "same", 6000, 500, g))
-        dout.copy_(torch.randint(-4, 5, (6000, 40), generator=g, device="cuda"))
+        ids.copy_(make_ids("skewed" if step % 2 else "same", 16_000, 500, g))
+        dout.copy_(torch.randint(-4, 5, (16_000, 40), generator=g, device="cuda"))
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(few.double(), grad_want(dout[:100], ids[:100], 500, 1.0))
@@ -234,7 +250,7 @@ def test_model_rows(dtype, k):
     g = rng(dtype * 10 + k)
     for side, table in ((M.P, P), (M.Q, Q)):
         rows = table.shape[0]
-        for count in (1, 700, 9000):
+        for count in (1, 700, 12_000):
             ids = make_ids("skewed", count, rows, g)
             assert torch.equal(M.rows(side, ids, k, scale=1.5), M.embed(table, ids, scale=1.5))
             dout = torch.randn(count, k, generator=g, device="cuda").to(table.dtype)
