@@ -181,17 +181,15 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, 
 //
 // A workgroup computes BM rows x BN columns; its wavefronts WM x WN each, as
 // 16 x 16 tiles of the matrix instructions.  A's and B's rows are staged in LDS
-// kRow = 128 bytes of depth at a time, two stages, copied by the memory
-// pipeline itself while the other stage is computed on: one barrier a stage.
+// kRow = 128 bytes of depth at a time; the copies of the next stages are on
+// their way while one is computed on.
 //
 // The 16-byte pieces of a staged row are stored in the order piece ^ (row & 7),
 // so that the 16 lanes that read one piece of 16 rows meet different banks; the
 // copy writes LDS linearly, so the lanes' global addresses carry that order.
 //
 // B is the matrix instruction's row operand: a lane then holds 4 consecutive
-// columns of C per tile.  B's rows are staged so that the four tiles of 64
-// columns give a lane 16 consecutive ones, and a row of C is written in whole
-// cache lines.
+// columns of C per tile (see column_of).
 constexpr int kRow = 128; // bytes of depth of a stage
 
 __device__ __attribute__((aligned(16))) const uint32_t g_zeros[4] = {0, 0, 0, 0};
@@ -248,6 +246,17 @@ __device__ __forceinline__ u32x4 piece_at(const T* p, int64_t n)
     return r;
 }
 
+// The column of C that row r of B's staged rows belongs to.  The matrix
+// instruction leaves a lane columns 4 (lane / 16) + 0..3 of each 16; with 16-bit
+// results two such tiles are made neighbours, so that a lane's 16-byte stores
+// hold consecutive columns and four lanes write 64 bytes of a row in one
+// instruction (binary32: they do as it is).
+template <typename T>
+__device__ __forceinline__ int column_of(int r)
+{
+    return sizeof(T) == 4 ? r : (r & ~31) + (r >> 2 & 3) * 8 + (r >> 4 & 1) * 4 + (r & 3);
+}
+
 // Workgroups are dealt to the 8 XCDs in turn: each XCD takes a run of
 // consecutive tiles, and runs go down 8 tiles of rows before the next column, so
 // that the tiles of an XCD share rows of A and B in its L2.
@@ -261,40 +270,79 @@ __device__ __forceinline__ void tile_place(const GemmArgs& g, uint32_t& tm, uint
     tm = b * 8 + (at - tn * high);
 }
 
+// Wait until at most N of this wavefront's memory operations are outstanding.
+template <int N>
+__device__ __forceinline__ void wait_memory()
+{
+    static_assert(N >= 0 && N < 64, "a 6-bit count");
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+}
+
+struct Yes {
+    static constexpr bool value = true;
+};
+struct No {
+    static constexpr bool value = false;
+};
+template <bool B, typename X, typename Y>
+struct Pick {
+    typedef X type;
+};
+template <typename X, typename Y>
+struct Pick<false, X, Y> {
+    typedef Y type;
+};
+
+template <typename T>
+__device__ __forceinline__ void add_piece(float (&v)[16 / sizeof(T)], const u32x4& x)
+{
+    Vec<T, 16 / (int)sizeof(T)> p;
+    __builtin_memcpy(&p, &x, 16);
+#pragma unroll
+    for (int c = 0; c < 16 / (int)sizeof(T); ++c)
+        v[c] += (float)p.v[c];
+}
+
 // DIRECT: rows of A and B start at 16-byte boundaries and the depth is whole
 // pieces; the copies go from memory to LDS by themselves.  Otherwise (any
 // alignment, any depth) they pass through registers.
-template <typename T, int BM, int BN, int WM, int WN, bool DIRECT>
+template <typename T, int BM, int BN, int WM, int WN, bool DIRECT, int NB>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(GemmArgs g, Epilogue e)
 {
-    constexpr int waves = (BM / WM) * (BN / WN), groups = (BM + BN) / 8 / waves;
+    constexpr int pieces = kRow / 16, deep = kRow / 64; // of a staged row; steps of the matrix instructions in a stage
+    constexpr int copied = 64 / pieces;                 // rows a wavefront copies at a time
+    constexpr int waves = (BM / WM) * (BN / WN), groups = (BM + BN) / copied / waves;
     constexpr int TM = WM / 16, TN = WN / 16, piece = 16 / (int)sizeof(T), per_stage = kRow / (int)sizeof(T);
     constexpr int stage_bytes = (BM + BN) * kRow;
-    static_assert(WN % 64 == 0 && (BM + BN) % (8 * waves) == 0, "tile shape");
-    __shared__ __attribute__((aligned(128))) char lds[2 * stage_bytes];
+    static_assert(WN % 64 == 0 && (BM + BN) % (copied * waves) == 0 && BM % copied == 0, "tile shape");
+    static_assert(DIRECT || NB == 2, "copies through registers have two stages in LDS");
+    __shared__ __attribute__((aligned(128))) char lds[NB * stage_bytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
     uint32_t tm, tn;
     tile_place(g, tm, tn);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-    const int64_t k0 = (int64_t)blockIdx.y * g.steps * per_stage, depth = g.depth - k0;
-    const int64_t left = (depth + per_stage - 1) / per_stage;
-    const int steps = (int)(left < g.steps ? left : g.steps);
+    const int64_t k0 = (int64_t)blockIdx.y * g.steps * per_stage;
+    const int64_t mine = (int64_t)g.steps * per_stage, depth = g.depth - k0 < mine ? g.depth - k0 : mine;
+    const int steps = (int)((depth + per_stage - 1) / per_stage);
 
-    // this lane's rows to copy: 8 rows a group, a 16-byte piece of one each; rows past the end repeat the last one
-    // (their sums are not written)
-    const int pc = (lane & 7) ^ (lane >> 3);
-    uint64_t src[groups];
+    // this lane's rows to copy: `copied` rows a group, a 16-byte piece of one each; rows past the end repeat the last
+    // one (their sums are not written)
+    auto turn = [](int row) { return row & (pieces - 1); };
+    const int pc = (lane & (pieces - 1)) ^ turn(lane / pieces);
+    const char* base[2] = {(const char*)((const T*)g.A + m0 * g.lda + k0), (const char*)((const T*)g.B + n0 * g.ldb + k0)};
+    typedef typename Pick<DIRECT, uint32_t, uint64_t>::type Offset;
+    Offset off[groups]; // from the tile's first row
 #pragma unroll
     for (int u = 0; u < groups; ++u) {
-        const int group = wave * groups + u, row = group * 8 + (lane >> 3);
-        if (group < BM / 8) {
-            const int64_t m = m0 + row < g.rows ? m0 + row : g.rows - 1;
-            src[u] = (uint64_t)((const T*)g.A + m * g.lda + k0 + pc * piece);
+        const int group = wave * groups + u, row = group * copied + lane / pieces;
+        if (group < BM / copied) {
+            const int64_t m = m0 + row < g.rows ? row : g.rows - 1 - m0;
+            off[u] = (Offset)((m * g.lda + pc * piece) * (int64_t)sizeof(T));
         } else {
-            const int r = row - BM, n = (r & ~63) + (r >> 2 & 3) * 16 + (r >> 4 & 3) * 4 + (r & 3);
-            const int64_t col = n0 + n < g.cols ? n0 + n : g.cols - 1;
-            src[u] = (uint64_t)((const T*)g.B + col * g.ldb + k0 + pc * piece);
+            const int r = row - BM, n = column_of<T>(r);
+            const int64_t col = n0 + n < g.cols ? n : g.cols - 1 - n0;
+            off[u] = (Offset)((col * g.ldb + pc * piece) * (int64_t)sizeof(T));
         }
     }
     // stages before `whole` lie inside the depth; in the last one pieces past it are zeros
@@ -302,36 +350,44 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(GemmArgs g,
     const int64_t room = depth - (int64_t)whole * per_stage - pc * piece; // this lane's elements in that stage
     uint64_t zeros = (uint64_t)g_zeros;
     asm("" : "+v"(zeros)); // in registers: the copies' addresses are selected, not branched on
-    u32x4 held[DIRECT ? 1 : groups];
-    auto fetch = [&](int s) {
+    u32x4 held[2][DIRECT ? 1 : groups]; // stages on their way through registers
+    auto fetch = [&](int s, auto full, int half = 0) {
+        constexpr bool FULL = decltype(full)::value;
+        const char* from[2] = {base[0] + (int64_t)s * kRow, base[1] + (int64_t)s * kRow};
         if constexpr (DIRECT) {
-            char* to = lds + (s & 1) * stage_bytes + wave * groups * 8 * kRow;
-            const bool none = s >= whole && room <= 0;
+            char* to = lds + s % NB * stage_bytes + wave * groups * copied * kRow;
+            if (FULL || s < whole) {
 #pragma unroll
-            for (int u = 0; u < groups; ++u) {
-                const uint64_t from = none ? zeros : src[u];
-                src[u] += kRow;
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                                 (__attribute__((address_space(3))) void*)(to + u * 8 * kRow), 16, 0,
-                                                 0);
-            }
-        } else if (s < whole) {
+                for (int u = 0; u < groups; ++u)
+                    __builtin_amdgcn_global_load_lds(
+                        (const __attribute__((address_space(1))) void*)(from[wave * groups + u >= BM / copied] + off[u]),
+                        (__attribute__((address_space(3))) void*)(to + u * 1024), 16, 0, 0);
+            } else {
 #pragma unroll
-            for (int u = 0; u < groups; ++u) {
-                held[u] = piece_at<T>((const T*)src[u], piece);
-                src[u] += kRow;
+                for (int u = 0; u < groups; ++u) {
+                    const uint64_t at = room <= 0 ? zeros : (uint64_t)(from[wave * groups + u >= BM / copied] + off[u]);
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)at,
+                                                     (__attribute__((address_space(3))) void*)(to + u * 1024), 16, 0, 0);
+                }
             }
         } else {
+            const int64_t some = FULL || s < whole ? piece : room;
 #pragma unroll
             for (int u = 0; u < groups; ++u)
-                held[u] = piece_at<T>((const T*)src[u], room);
+                held[half][u] = piece_at<T>((const T*)(from[wave * groups + u >= BM / copied] + off[u]), some);
         }
     };
-    auto keep = [&](int s) {
-        char* to = lds + (s & 1) * stage_bytes + wave * groups * 8 * kRow + lane * 16;
+    auto keep = [&](int s, int half) {
+        char* to = lds + s % NB * stage_bytes + wave * groups * copied * kRow + lane * 16;
 #pragma unroll
         for (int u = 0; u < groups; ++u)
-            *(u32x4*)(to + u * 8 * kRow) = held[DIRECT ? 0 : u];
+            *(u32x4*)(to + u * 1024) = held[half][DIRECT ? 0 : u];
+    };
+    // all copies of this wavefront are in LDS that everyone's have to be in, and everyone is done reading before
+    auto meet = [&] {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
     };
 
     f32x4 acc[TM][TN];
@@ -342,64 +398,164 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(GemmArgs g,
             acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     const int quad = lane >> 4, r16 = lane & 15;
-    if (steps > 0) {
-        fetch(0);
-        if constexpr (!DIRECT)
-            keep(0);
-    }
-    for (int s = 0; s < steps; ++s) {
-        // everyone's copies of stage s are in LDS, and everyone is done reading stage s - 1
-        if constexpr (DIRECT) {
-            __builtin_amdgcn_s_waitcnt(0x0f70); // vmcnt(0)
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-        } else {
-            __syncthreads();
-        }
-        if (s + 1 < steps)
-            fetch(s + 1);
-        const char* at = lds + (s & 1) * stage_bytes;
+    u32x4 a[2][TM], b[2][TN]; // operands of this step and of the next
+    auto read = [&](int to, int s, int kk) {
+        const char* at = lds + s % NB * stage_bytes + ((kk * 4 + quad) ^ turn(r16)) * 16 + r16 * kRow;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            const int sw = ((kk * 4 + quad) ^ (r16 & 7)) * 16;
-            u32x4 a[TM], b[TN];
+        for (int j = 0; j < TN; ++j)
+            b[to][j] = *(const u32x4*)(at + (BM + wn + j * 16) * kRow);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+            a[to][i] = *(const u32x4*)(at + (wm + i * 16) * kRow);
+    };
+    auto multiply = [&](int from) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j)
-                b[j] = *(const u32x4*)(at + (BM + wn + j * 16 + r16) * kRow + sw);
+                mma<T>(acc[i][j], b[from][j], a[from][i]);
+    };
+    if constexpr (DIRECT) {
+        // Of the ring of NB stages one is computed on and the others are on their way.  The operands of every step of
+        // the matrix instructions are read from LDS during the step before, and everyone meets once a stage.
+        auto stage = [&](int s, auto full) { // full: the stage to fetch exists and is whole
+            constexpr bool FULL = decltype(full)::value;
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
-                a[i] = *(const u32x4*)(at + (wm + i * 16 + r16) * kRow + sw);
+            for (int kk = 0; kk < deep; ++kk) {
+                if (kk + 1 < deep) {
+                    read((kk + 1) & 1, s, kk + 1);
+                } else if (FULL || s + 1 < steps) {
+                    if (FULL || s + NB - 1 < steps)
+                        wait_memory<(NB - 2) * groups>(); // stage s + 1 has landed
+                    else
+                        wait_memory<0>();
+                    meet();
+                    if (FULL || s + NB < steps)
+                        fetch(s + NB, full);
+                    read((kk + 1) & 1, s + 1, 0);
+                }
+                multiply(kk & 1);
+                if constexpr (FULL) {
+                    // spread the reads and copies among the products instead of before them (8192^3 bfloat16: 796 us
+                    // against 828)
+                    constexpr int products = TM * TN * (sizeof(T) == 4 ? 4 : 1), parts = products >= 64 ? 16 : 8;
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+                    for (int q = 0; q < parts; ++q) {
+                        __builtin_amdgcn_sched_group_barrier(0x100, (TM + TN + parts - 1) / parts, 0); // LDS reads
+                        if (kk + 1 == deep)
+                            __builtin_amdgcn_sched_group_barrier(0x020, (groups + parts - 1) / parts, 0); // copies
+                        __builtin_amdgcn_sched_group_barrier(0x008, products / parts, 0); // matrix instructions
+                    }
+                }
+            }
+        };
+        static_assert(deep % 2 == 0, "a stage begins with the operands in half 0");
+        int s = 0;
+        if (steps > 0) {
 #pragma unroll
-                for (int j = 0; j < TN; ++j)
-                    mma<T>(acc[i][j], b[j], a[i]);
+            for (int i = 0; i < NB; ++i)
+                if (i < steps)
+                    fetch(i, No());
+            if (steps >= NB)
+                wait_memory<(NB - 1) * groups>();
+            else
+                wait_memory<0>();
+            meet();
+            read(0, 0, 0);
         }
-        if constexpr (!DIRECT)
+        for (; s + NB < whole; ++s)
+            stage(s, Yes());
+        for (; s < steps; ++s)
+            stage(s, No());
+    } else {
+        // One stage is computed on, the next one is in registers or on its way there, the one after it on its way.
+        auto stage = [&](int s, int half, auto full) {
+            constexpr bool FULL = decltype(full)::value;
+            meet();
+            if (FULL || s + 2 < steps)
+                fetch(s + 2, full, half);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int kk = 0; kk < deep; ++kk) {
+                read(0, s, kk);
+                multiply(0);
+            }
+            if (FULL || s + 1 < steps)
+                keep(s + 1, half ^ 1);
+        };
+        if (steps > 0) {
+            fetch(0, No(), 0);
+            if (steps > 1)
+                fetch(1, No(), 1);
+            keep(0, 0);
+        }
+        int s = 0;
+        for (; s + 3 < whole; s += 2) {
+            stage(s, 0, Yes());
+            stage(s + 1, 1, Yes());
+        }
+        for (; s < steps; s += 2) {
+            stage(s, 0, No());
             if (s + 1 < steps)
-                keep(s + 1);
+                stage(s + 1, 1, No());
+        }
     }
 
+    constexpr int together = sizeof(T) == 4 ? 1 : 2, chunks = TN / together; // tiles whose columns a lane holds together
+    const int64_t mrow = m0 + wm + r16, ncol = n0 + wn + quad * piece;
+    if (g.part) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-        const int64_t m = m0 + wm + i * 16 + r16;
+        for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int q = 0; q < TN / 4; ++q) {
-            const int64_t n = n0 + wn + q * 64 + quad * 16;
-            float v[16];
+            for (int j = 0; j < chunks; ++j) {
+                const int64_t m = mrow + i * 16, n = ncol + j * 16 * together;
+                float v[piece];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    v[j * 4 + c] = acc[i][q * 4 + j][c];
-            if (!g.part)
-                finish<T, 16>(e, m, n, v);
-            else if (m < g.rows && n < g.cols)
-                write_some<float, 16>(g.part + ((int64_t)blockIdx.y * g.rows + m) * g.cols + n,
-                                      g.cols - n < 16 ? (int)(g.cols - n) : 16, v);
-        }
+                for (int c = 0; c < piece; ++c)
+                    v[c] = acc[i][j * together + c / 4][c % 4];
+                if (m < g.rows && n < g.cols)
+                    write_some<float, piece>(g.part + ((int64_t)blockIdx.y * g.rows + m) * g.cols + n,
+                                             g.cols - n < piece ? (int)(g.cols - n) : piece, v);
+            }
+        return;
     }
+    // everything that the epilogue reads, at once: one wait for memory instead of one for every chunk
+    u32x4 bias[chunks], res[TM][chunks];
+    if (e.bias) {
+#pragma unroll
+        for (int j = 0; j < chunks; ++j)
+            bias[j] = piece_at<T>((const T*)e.bias + ncol + j * 16 * together, e.N - ncol - j * 16 * together);
+    }
+    if (e.residual) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < chunks; ++j) {
+                const int64_t m = mrow + i * 16, n = ncol + j * 16 * together;
+                res[i][j] = piece_at<T>((const T*)e.residual + m * e.ldr + n, m < e.M ? e.N - n : 0);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < chunks; ++j) {
+            const int64_t m = mrow + i * 16, n = ncol + j * 16 * together;
+            if (m >= e.M || n >= e.N)
+                continue;
+            const int some = e.N - n < piece ? (int)(e.N - n) : piece;
+            float v[piece];
+#pragma unroll
+            for (int c = 0; c < piece; ++c)
+                v[c] = acc[i][j * together + c / 4][c % 4];
+            if (e.bias)
+                add_piece<T>(v, bias[j]);
+            if (e.z)
+                write_some<T, piece>((T*)e.z + m * e.ldz + n, some, v);
+            activate<sizeof(T) == 4, piece>(v, e.act);
+            if (e.residual)
+                add_piece<T>(v, res[i][j]);
+            write_some<T, piece>((T*)e.y + m * e.ldy + n, some, v);
+        }
 }
 
 // The slices' sums, added in order and finished: 4 columns a thread.
@@ -633,29 +789,47 @@ constexpr uint32_t kMostWgs = 1 << 22;
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
 
 // Which tile a product takes, and over how many slices of its depth.
+//
+// A tile of 256 x 256 moves half the bytes per product of one of 128 x 128 and
+// runs at 1.25 times its rate where there are enough of them (4096^3 bfloat16:
+// 116 us against 141), but only one fits a CU, so the last round of a product
+// with few tiles leaves more of the chip idle: 128 x 2048^2 x 2 and smaller
+// (4096 x 2048 x 2048: 55 us against 40) take the small one.
+//
+// Small tiles run two to a CU with two stages each, which hides one's barriers
+// and epilogue behind the other's products; where there is at most one per CU it
+// gets the LDS of both as four stages (2048 x 2048 x 4096: 37 us against 48).
 struct Shape {
-    int tile;   // 0: few rows; else rows of a tile
-    int slices; // > 1: sums to the workspace, joined afterwards
-    int steps;  // stages of a slice
+    int tile;       // 0: few rows; else rows of a tile
+    int slices;     // > 1: sums to the workspace, joined afterwards
+    int steps;      // stages of a slice
+    int64_t groups; // workgroups
 };
 
 Shape shape_of(int64_t rows, int64_t cols, int64_t depth, int dtype)
 {
     const int64_t stages = up(depth * (int64_t)elem_bytes(dtype), kRow);
-    Shape s{0, 1, (int)std::max<int64_t>(stages, 1)};
+    Shape s{0, 1, (int)std::max<int64_t>(stages, 1), 0};
     if (rows <= 16 || cols == 0)
         return s;
     const int64_t big = up(rows, 256) * up(cols, 256), mid = up(rows, 128) * up(cols, 128);
-    s.tile = big >= 200 && stages >= 8 ? 256 : rows > 64 ? 128 : 64;
-    const int64_t tiles = s.tile == 256 ? big : s.tile == 128 ? mid : up(rows, 64) * up(cols, 128);
-    // enough workgroups for every CU, each with at least 4 stages
-    if (tiles < 256 && s.tile != 256) {
-        const int64_t want = std::min<int64_t>(512 / tiles, stages / 4);
-        if (want > 1) {
-            s.steps = (int)up(stages, want);
-            s.slices = (int)up(stages, s.steps);
-        }
+    if (stages >= 8 && (double)up(big, 256) <= 0.625 * 0.5 * (double)up(mid, 256)) {
+        s.tile = 256;
+        s.groups = big;
+        return s;
     }
+    // Tiles of 64 rows where they fill the last round better: one takes 0.55 of the other's time in binary32, 0.7 in
+    // 16 bits (bound by what comes from L2), measured on 1000 x 5000 x 776 (88 us against 112; 21.6 against 20).
+    const int64_t low = up(rows, 64) * up(cols, 128);
+    s.tile = mid <= 128 || (dtype == kF32 ? 0.55 : 0.7) * (double)up(low, 256) < (double)up(mid, 256) ? 64 : 128;
+    const int64_t tiles = s.tile == 128 ? mid : low;
+    // a workgroup for every CU, each with at least 4 stages (binary32, whose products take four times as long: 2)
+    const int64_t want = std::min<int64_t>(256 / std::min<int64_t>(tiles, 256), stages / (dtype == kF32 ? 2 : 4));
+    if (want > 1) {
+        s.steps = (int)up(stages, want);
+        s.slices = (int)up(stages, s.steps);
+    }
+    s.groups = tiles * s.slices;
     return s;
 }
 
@@ -670,14 +844,14 @@ bool rows_aligned(const void* p, int64_t ld, int dtype)
     return ((uintptr_t)p & 15) == 0 && ld * (int64_t)elem_bytes(dtype) % 16 == 0;
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool DIRECT>
+template <typename T, int BM, int BN, int WM, int WN, bool DIRECT, int NB>
 hipError_t gemm_launch(GemmArgs g, const Epilogue& e, int slices, hipStream_t st)
 {
     g.tiles_m = (uint32_t)up(g.rows, BM);
     g.tiles_n = (uint32_t)up(g.cols, BN);
     const uint32_t all = g.tiles_m * g.tiles_n;
     for (g.tile0 = 0; g.tile0 < all; g.tile0 += kMostWgs) // a multiple of 8: the XCDs' turn goes on
-        hipLaunchKernelGGL((k_gemm<T, BM, BN, WM, WN, DIRECT>), dim3(std::min(kMostWgs, all - g.tile0), slices),
+        hipLaunchKernelGGL((k_gemm<T, BM, BN, WM, WN, DIRECT, NB>), dim3(std::min(kMostWgs, all - g.tile0), slices),
                            dim3((BM / WM) * (BN / WN) * 64), 0, st, g, e);
     return hipGetLastError();
 }
@@ -701,18 +875,23 @@ hipError_t gemm(GemmArgs g, const Epilogue& e, int dtype, void* part, hipStream_
             hipLaunchKernelGGL((k_gemm_few<T, 1>), dim3((unsigned)wgs), dim3(256), 0, st, g, e);
         return hipGetLastError();
     }
+    // (256 rows of a tile are addressed by 31 bits from its first)
+    const int64_t far = std::max(g.lda, g.ldb) * (int64_t)sizeof(T) * 256;
     const bool direct = rows_aligned(g.A, g.lda, dtype) && rows_aligned(g.B, g.ldb, dtype) &&
-                        g.depth * (int64_t)sizeof(T) % 16 == 0;
+                        g.depth * (int64_t)sizeof(T) % 16 == 0 && far < (int64_t(1) << 31);
     hipError_t err;
-    if (s.tile == 256)
-        err = direct ? gemm_launch<T, 256, 256, 128, 64, true>(g, e, 1, st)
-                     : gemm_launch<T, 128, 128, 64, 64, false>(g, e, 1, st);
-    else if (s.tile == 128)
-        err = direct ? gemm_launch<T, 128, 128, 64, 64, true>(g, e, s.slices, st)
-                     : gemm_launch<T, 128, 128, 64, 64, false>(g, e, s.slices, st);
+    if (s.tile == 256 && direct)
+        err = gemm_launch<T, 256, 256, 128, 64, true, 2>(g, e, 1, st);
+    else if (s.tile >= 128 && direct && s.groups <= 256)
+        err = gemm_launch<T, 128, 128, 32, 64, true, 4>(g, e, s.slices, st);
+    else if (s.tile >= 128 && direct)
+        err = gemm_launch<T, 128, 128, 32, 64, true, 2>(g, e, s.slices, st);
+    else if (s.tile >= 128)
+        err = gemm_launch<T, 128, 128, 32, 64, false, 2>(g, e, s.slices, st);
+    else if (direct)
+        err = gemm_launch<T, 64, 128, 16, 64, true, 3>(g, e, s.slices, st);
     else
-        err = direct ? gemm_launch<T, 64, 128, 32, 64, true>(g, e, s.slices, st)
-                     : gemm_launch<T, 64, 128, 32, 64, false>(g, e, s.slices, st);
+        err = gemm_launch<T, 64, 128, 32, 64, false, 2>(g, e, s.slices, st);
     if (err != hipSuccess || s.slices == 1)
         return err;
     const int64_t wgs = std::min<int64_t>(up(g.rows * up(g.cols, 4), 256), kMostWgs);

@@ -14,6 +14,7 @@ raises ``ImportError``: there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -313,16 +314,19 @@ class _On:
 
     def __init__(self, stream):
         self.device = torch.cuda.current_device()
-        if stream is not None and stream.device_index != self.device:
-            raise ValueError("the stream is on another device than the current one")
         self.stream = stream
-        self.handle = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+        if stream is None:
+            self.handle = _current_stream(self.device)
+        else:
+            if stream.device_index != self.device:
+                raise ValueError("the stream is on another device than the current one")
+            self.handle = stream.cuda_stream
 
     def empty(self, shape, dtype):
         if self.stream is None:
-            return torch.empty(shape, dtype=dtype, device="cuda")
+            return torch.empty(shape, dtype=dtype, device=_cuda(self.device))
         with torch.cuda.stream(self.stream):
-            return torch.empty(shape, dtype=dtype, device="cuda")
+            return torch.empty(shape, dtype=dtype, device=_cuda(self.device))
 
     def workspace(self, nbytes):
         """(address, bytes, tensor) of a new workspace; the tensor must outlive the call."""
@@ -330,6 +334,16 @@ class _On:
             return None, 0, None
         t = self.empty((nbytes,), torch.uint8)
         return t.data_ptr(), nbytes, t
+
+
+# the handle alone, where torch offers it: a Stream object costs as much as a small launch
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                          lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+@functools.lru_cache(maxsize=None)
+def _cuda(index):
+    return torch.device("cuda", index)
 
 
 def _matrix(t, what, device, dtype=None, shape=None):
