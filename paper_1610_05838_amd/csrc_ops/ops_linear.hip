@@ -107,6 +107,7 @@ struct Epilogue {
     void *y, *z;
     int64_t ldr, ldy, ldz, M, N;
     int act;
+    bool near; // 256 rows of each matrix are addressed by 31 bits
 };
 
 // C elements at p of which the first `n` exist (zeros for the rest).
@@ -519,43 +520,68 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(GemmArgs g,
             }
         return;
     }
-    // everything that the epilogue reads, at once: one wait for memory instead of one for every chunk
-    u32x4 bias[chunks], res[TM][chunks];
-    if (e.bias) {
-#pragma unroll
-        for (int j = 0; j < chunks; ++j)
-            bias[j] = piece_at<T>((const T*)e.bias + ncol + j * 16 * together, e.N - ncol - j * 16 * together);
-    }
-    if (e.residual) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < chunks; ++j) {
-                const int64_t m = mrow + i * 16, n = ncol + j * 16 * together;
-                res[i][j] = piece_at<T>((const T*)e.residual + m * e.ldr + n, m < e.M ? e.N - n : 0);
+    // What the epilogue reads, several pieces at a time: one wait for memory instead of one a piece.  A tile that lies
+    // inside C needs no checks, and its addresses are a scalar and a 32-bit offset of the lane: where the output is
+    // most of the work the vector instructions of an epilogue with them took as long as its stores.
+    auto epilogue = [&](auto inside) {
+        constexpr bool INSIDE = decltype(inside)::value;
+        constexpr int batch = TM * chunks <= 8 ? TM : 8 / chunks;
+        const int lrow = wm + r16, lcol = wn + quad * piece;
+        // piece (i, j) of a matrix of pitch ld
+        auto at = [&](const void* p, int64_t ld, int i, int j) {
+            const int far = i * 16, near = j * 16 * together;
+            if (INSIDE) {
+                const T* tile = (const T*)p + (m0 + far) * ld + n0 + near;
+                return (T*)((char*)tile + (uint32_t)(lrow * (uint32_t)ld + lcol) * (uint32_t)sizeof(T));
             }
-    }
+            return (T*)p + (mrow + far) * ld + ncol + near;
+        };
+        u32x4 bias[chunks];
+        if (e.bias) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < chunks; ++j) {
-            const int64_t m = mrow + i * 16, n = ncol + j * 16 * together;
-            if (m >= e.M || n >= e.N)
-                continue;
-            const int some = e.N - n < piece ? (int)(e.N - n) : piece;
-            float v[piece];
-#pragma unroll
-            for (int c = 0; c < piece; ++c)
-                v[c] = acc[i][j * together + c / 4][c % 4];
-            if (e.bias)
-                add_piece<T>(v, bias[j]);
-            if (e.z)
-                write_some<T, piece>((T*)e.z + m * e.ldz + n, some, v);
-            activate<sizeof(T) == 4, piece>(v, e.act);
-            if (e.residual)
-                add_piece<T>(v, res[i][j]);
-            write_some<T, piece>((T*)e.y + m * e.ldy + n, some, v);
+            for (int j = 0; j < chunks; ++j)
+                bias[j] = piece_at<T>(at(e.bias, 0, 0, j), INSIDE ? piece : e.N - ncol - j * 16 * together);
         }
+#pragma unroll
+        for (int i0 = 0; i0 < TM; i0 += batch) {
+            u32x4 res[batch][chunks];
+            if (e.residual) {
+#pragma unroll
+                for (int i = 0; i < batch; ++i)
+#pragma unroll
+                    for (int j = 0; j < chunks; ++j)
+                        res[i][j] = piece_at<T>(at(e.residual, e.ldr, i0 + i, j),
+                                                INSIDE                            ? piece
+                                                : mrow + (i0 + i) * 16 < e.M ? e.N - ncol - j * 16 * together
+                                                                                  : 0);
+            }
+#pragma unroll
+            for (int i = 0; i < batch; ++i)
+#pragma unroll
+                for (int j = 0; j < chunks; ++j) {
+                    const int64_t m = mrow + (i0 + i) * 16, n = ncol + j * 16 * together;
+                    if (!INSIDE && (m >= e.M || n >= e.N))
+                        continue;
+                    const int some = INSIDE || e.N - n >= piece ? piece : (int)(e.N - n);
+                    float v[piece];
+#pragma unroll
+                    for (int c = 0; c < piece; ++c)
+                        v[c] = acc[i0 + i][j * together + c / 4][c % 4];
+                    if (e.bias)
+                        add_piece<T>(v, bias[j]);
+                    if (e.z)
+                        write_some<T, piece>(at(e.z, e.ldz, i0 + i, j), some, v);
+                    activate<sizeof(T) == 4, piece>(v, e.act);
+                    if (e.residual)
+                        add_piece<T>(v, res[i][j]);
+                    write_some<T, piece>(at(e.y, e.ldy, i0 + i, j), some, v);
+                }
+        }
+    };
+    if (e.near && m0 + BM <= e.M && n0 + BN <= e.N)
+        epilogue(Yes());
+    else
+        epilogue(No());
 }
 
 // The slices' sums, added in order and finished: 4 columns a thread.
@@ -839,6 +865,9 @@ size_t part_bytes(int64_t rows, int64_t cols, int64_t depth, int dtype)
     return s.slices > 1 ? round256(sizeof(float) * (size_t)s.slices * (size_t)rows * (size_t)cols) : 0;
 }
 
+// 256 rows are addressed by 31 bits from the first.
+bool near(int64_t ld, int dtype) { return ld * (int64_t)elem_bytes(dtype) * 257 < (int64_t(1) << 31); }
+
 bool rows_aligned(const void* p, int64_t ld, int dtype)
 {
     return ((uintptr_t)p & 15) == 0 && ld * (int64_t)elem_bytes(dtype) % 16 == 0;
@@ -875,10 +904,8 @@ hipError_t gemm(GemmArgs g, const Epilogue& e, int dtype, void* part, hipStream_
             hipLaunchKernelGGL((k_gemm_few<T, 1>), dim3((unsigned)wgs), dim3(256), 0, st, g, e);
         return hipGetLastError();
     }
-    // (256 rows of a tile are addressed by 31 bits from its first)
-    const int64_t far = std::max(g.lda, g.ldb) * (int64_t)sizeof(T) * 256;
     const bool direct = rows_aligned(g.A, g.lda, dtype) && rows_aligned(g.B, g.ldb, dtype) &&
-                        g.depth * (int64_t)sizeof(T) % 16 == 0 && far < (int64_t(1) << 31);
+                        g.depth * (int64_t)sizeof(T) % 16 == 0 && near(std::max(g.lda, g.ldb), dtype);
     hipError_t err;
     if (s.tile == 256 && direct)
         err = gemm_launch<T, 256, 256, 128, 64, true, 2>(g, e, 1, st);
@@ -904,7 +931,8 @@ template <typename T>
 hipError_t linear_typed(const LinearLaunch& a, hipStream_t st)
 {
     GemmArgs g{a.x, a.w, a.ldx, a.ldw, a.M, a.N, a.K, 0, 0, 0, 0, nullptr};
-    const Epilogue e{a.bias, a.residual, a.y, a.z, a.ldr, a.ldy, a.ldz, a.M, a.N, a.act};
+    const Epilogue e{a.bias, a.residual, a.y, a.z, a.ldr, a.ldy, a.ldz, a.M, a.N, a.act,
+                     near(std::max(a.ldr, std::max(a.ldy, a.ldz)), a.dtype)};
     return gemm<T>(g, e, a.dtype, a.work, st);
 }
 
@@ -964,12 +992,14 @@ hipError_t grad_typed(const LinearGradLaunch& a, hipStream_t st)
         GemmArgs g{as_is ? a.dy : w.dz, w.w_t, as_is ? a.lddy : w.Np, w.Np, a.M, a.K, a.N, 0, 0, 0, 0, nullptr};
         if (!as_is)
             g.depth = w.Np; // the zeros behind a row are part of it: whole pieces
-        const Epilogue e{nullptr, nullptr, a.dx, nullptr, 0, a.lddx, 0, a.M, a.K, kNone};
+        const Epilogue e{nullptr, nullptr, a.dx, nullptr, 0, a.lddx, 0, a.M, a.K, kNone,
+                         near(a.lddx, a.dtype)};
         err = gemm<T>(g, e, a.dtype, w.part, st);
     }
     if (a.dw && err == hipSuccess) {
         GemmArgs g{w.dz_t, w.x_t, w.Mp, w.Mp, a.N, a.K, w.Mp, 0, 0, 0, 0, nullptr};
-        const Epilogue e{nullptr, nullptr, a.dw, nullptr, 0, a.lddw, 0, a.N, a.K, kNone};
+        const Epilogue e{nullptr, nullptr, a.dw, nullptr, 0, a.lddw, 0, a.N, a.K, kNone,
+                         near(a.lddw, a.dtype)};
         err = gemm<T>(g, e, a.dtype, w.part, st);
     }
     if (a.dbias && a.N && err == hipSuccess) {
