@@ -199,9 +199,22 @@ struct GemmArgs {
     const void *A, *B;
     int64_t lda, ldb, rows, cols, depth;
     uint32_t tiles_m, tiles_n, tile0; // of the whole product; this launch's first
-    int steps;                        // stages of one workgroup: a slice of the depth, blockIdx.y
+    int steps;                        // stages of one workgroup: a slice of the depth
     float* part;                      // the slices' sums [slice][rows][cols], or nullptr: one slice, finished here
 };
+
+// One launch's work: a product's tiles, slice by slice, the ids of a slice
+// rounded up to whole turns of the XCDs; from id `second` on another product's;
+// from id `sums` on the column sums of dZ (see k_turn).
+struct Products {
+    GemmArgs g[2];
+    Epilogue e[2];
+    uint32_t second, sums;
+    const float* col_sums;
+    int64_t row_tiles, cols;
+    void* dbias;
+};
+constexpr uint32_t kNoWork = 0xffffffffu;
 
 template <typename T>
 __device__ __forceinline__ void mma(f32x4& c, const u32x4& b, const u32x4& a);
@@ -261,9 +274,9 @@ __device__ __forceinline__ int column_of(int r)
 // Workgroups are dealt to the 8 XCDs in turn: each XCD takes a run of
 // consecutive tiles, and runs go down 8 tiles of rows before the next column, so
 // that the tiles of an XCD share rows of A and B in its L2.
-__device__ __forceinline__ void tile_place(const GemmArgs& g, uint32_t& tm, uint32_t& tn)
+__device__ __forceinline__ void tile_place(const GemmArgs& g, uint32_t id, uint32_t& tm, uint32_t& tn)
 {
-    const uint32_t all = g.tiles_m * g.tiles_n, id = blockIdx.x + g.tile0, x = id & 7;
+    const uint32_t all = g.tiles_m * g.tiles_n, x = id & 7;
     const uint32_t t = x * (all >> 3) + (x < (all & 7) ? x : all & 7) + (id >> 3);
     const uint32_t band = 8 * g.tiles_n, b = t / band, at = t - b * band;
     const uint32_t high = g.tiles_m - b * 8 < 8 ? g.tiles_m - b * 8 : 8;
@@ -304,11 +317,41 @@ __device__ __forceinline__ void add_piece(float (&v)[16 / sizeof(T)], const u32x
         v[c] += (float)p.v[c];
 }
 
+// dbias from the column sums per 64 rows, 64 columns a workgroup of `parts`
+// wavefronts: each adds a consecutive part of the tiles, the sums are joined in
+// order.
+template <typename T, int PARTS>
+__device__ __forceinline__ void add_columns(const Products& p, int64_t block, float* lds)
+{
+    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
+    const int64_t c = block * 64 + x, each = (p.row_tiles + PARTS - 1) / PARTS;
+    const int64_t from = y * each, to = from + each < p.row_tiles ? from + each : p.row_tiles;
+    float sum = 0.0f;
+    if (c < p.cols)
+        for (int64_t t0 = from; t0 < to; t0 += 8) {
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                v[u] = t0 + u < to ? p.col_sums[(t0 + u) * p.cols + c] : 0.0f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                sum += v[u];
+        }
+    lds[y * 64 + x] = sum;
+    __syncthreads();
+    if (y == 0 && c < p.cols) {
+#pragma unroll
+        for (int w = 1; w < PARTS; ++w)
+            sum += lds[w * 64 + x];
+        ((T*)p.dbias)[c] = T(sum);
+    }
+}
+
 // DIRECT: rows of A and B start at 16-byte boundaries and the depth is whole
 // pieces; the copies go from memory to LDS by themselves.  Otherwise (any
 // alignment, any depth) they pass through registers.
 template <typename T, int BM, int BN, int WM, int WN, bool DIRECT, int NB>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(GemmArgs g, Epilogue e)
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(Products p)
 {
     constexpr int pieces = kRow / 16, deep = kRow / 64; // of a staged row; steps of the matrix instructions in a stage
     constexpr int copied = 64 / pieces;                 // rows a wavefront copies at a time
@@ -320,10 +363,22 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(GemmArgs g,
     __shared__ __attribute__((aligned(128))) char lds[NB * stage_bytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
-    uint32_t tm, tn;
-    tile_place(g, tm, tn);
+    if (blockIdx.x >= p.sums) {
+        add_columns<T, waves>(p, blockIdx.x - p.sums, (float*)lds);
+        return;
+    }
+    const bool other = blockIdx.x >= p.second;
+    const GemmArgs g = other ? p.g[1] : p.g[0];
+    const Epilogue e = other ? p.e[1] : p.e[0];
+    const uint32_t ids = (g.tiles_m * g.tiles_n + 7) & ~7u;
+    uint32_t id = blockIdx.x + g.tile0 - (other ? p.second : 0), tm, tn;
+    const uint32_t slice = g.part ? id / ids : 0;
+    id -= slice * ids;
+    if (id >= g.tiles_m * g.tiles_n)
+        return;
+    tile_place(g, id, tm, tn);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-    const int64_t k0 = (int64_t)blockIdx.y * g.steps * per_stage;
+    const int64_t k0 = (int64_t)slice * g.steps * per_stage;
     const int64_t mine = (int64_t)g.steps * per_stage, depth = g.depth - k0 < mine ? g.depth - k0 : mine;
     const int steps = (int)((depth + per_stage - 1) / per_stage);
 
@@ -515,7 +570,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(GemmArgs g,
                 for (int c = 0; c < piece; ++c)
                     v[c] = acc[i][j * together + c / 4][c % 4];
                 if (m < g.rows && n < g.cols)
-                    write_some<float, piece>(g.part + ((int64_t)blockIdx.y * g.rows + m) * g.cols + n,
+                    write_some<float, piece>(g.part + ((int64_t)slice * g.rows + m) * g.cols + n,
                                              g.cols - n < piece ? (int)(g.cols - n) : piece, v);
             }
         return;
@@ -584,14 +639,29 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(GemmArgs g,
         epilogue(No());
 }
 
-// The slices' sums, added in order and finished: 4 columns a thread.
+// The slices' sums, added in order and finished: 4 columns a thread.  From
+// workgroup `second` on another product's.
+struct Join {
+    const float* part[2];
+    int slices[2];
+    int64_t rows[2], cols[2];
+    Epilogue e[2];
+    uint32_t second;
+};
+
 template <typename T>
-__global__ __launch_bounds__(256) void k_gemm_join(const float* __restrict__ part, int slices, int64_t rows,
-                                                   int64_t cols, Epilogue e)
+__global__ __launch_bounds__(256) void k_gemm_join(Join p)
 {
+    const bool other = blockIdx.x >= p.second;
+    const float* part = other ? p.part[1] : p.part[0];
+    const int slices = other ? p.slices[1] : p.slices[0];
+    const int64_t rows = other ? p.rows[1] : p.rows[0], cols = other ? p.cols[1] : p.cols[0];
+    const Epilogue e = other ? p.e[1] : p.e[0];
+    const uint32_t block = other ? blockIdx.x - p.second : blockIdx.x;
+    const uint32_t blocks = other || p.second > gridDim.x ? gridDim.x - (other ? p.second : 0) : p.second;
     const int64_t per_row = (cols + 3) / 4, all = rows * per_row, size = rows * cols;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int64_t m = i / per_row, n = (i - m * per_row) * 4;
+    for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < all; i += (int64_t)blocks * 256) {
+        const int64_t m = all <= 0xffffffff ? (uint32_t)i / (uint32_t)per_row : i / per_row, n = (i - m * per_row) * 4;
         const int some = cols - n < 4 ? (int)(cols - n) : 4;
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int s0 = 0; s0 < slices; s0 += 4) {
@@ -675,6 +745,14 @@ __global__ __launch_bounds__(256) void k_gemm_few(GemmArgs g, Epilogue e)
     }
 }
 
+// The column sums alone.
+template <typename T>
+__global__ __launch_bounds__(512) void k_dbias(Products p)
+{
+    __shared__ float lds[8 * 64];
+    add_columns<T, 8>(p, blockIdx.x, lds);
+}
+
 // ------------------------------------------------- operands of the gradient
 //
 // dX sums over the columns of dZ, dW over its rows, so W, dZ and X are also
@@ -702,37 +780,45 @@ struct Turns {
     int64_t tiles;
 };
 
+constexpr int kTurnThreads = 512;
+
 template <typename T>
-__global__ __launch_bounds__(256) void k_turn(Turns a)
+__global__ __launch_bounds__(kTurnThreads) void k_turn(Turns a)
 {
-    constexpr int V = 16 / (int)sizeof(T), across = 64 / V, down = 256 / across, turns = 64 / down;
+    constexpr int V = 16 / (int)sizeof(T), across = 64 / V, down = kTurnThreads / across, turns = 64 / down;
     __shared__ T tile[64][64 + 4 / sizeof(T) * 1];
     __shared__ float sums[down][64];
     const int tx = threadIdx.x % across, ty = threadIdx.x / across;
     for (int64_t id0 = blockIdx.x; id0 < a.tiles; id0 += gridDim.x) {
         int which = 0;
-        int64_t id = id0;
+        uint32_t id = (uint32_t)id0;
         while (which < 2 && id >= a.job[which].tiles)
-            id -= a.job[which++].tiles;
+            id -= (uint32_t)a.job[which++].tiles;
         const Turn& j = a.job[which];
-        const int64_t wide = (j.cols + 63) / 64, tr = id / wide, r0 = tr * 64, c0 = (id - tr * wide) * 64;
+        const uint32_t wide = (uint32_t)((j.cols + 63) / 64);
+        const int64_t tr = id / wide, r0 = tr * 64, c0 = (int64_t)(id - (uint32_t)tr * wide) * 64;
         const int64_t c = c0 + tx * V;
         float sum[V];
 #pragma unroll
         for (int i = 0; i < V; ++i)
             sum[i] = 0.0f;
+        u32x4 raw[turns], rz[turns];
 #pragma unroll
         for (int u = 0; u < turns; ++u) {
-            const int64_t r = r0 + ty + u * down;
-            const int64_t some = r < j.rows ? j.cols - c : 0;
-            const u32x4 raw = piece_at<T>((const T*)j.src + r * j.ld + c, some);
+            const int64_t r = r0 + ty + u * down, some = r < j.rows ? j.cols - c : 0;
+            raw[u] = piece_at<T>((const T*)j.src + r * j.ld + c, some);
+            if (which == 0 && a.act != kNone)
+                rz[u] = piece_at<T>((const T*)a.z + r * a.ldz + c, some);
+        }
+#pragma unroll
+        for (int u = 0; u < turns; ++u) {
+            const int64_t r = r0 + ty + u * down, some = r < j.rows ? j.cols - c : 0;
             Vec<T, V> x;
-            __builtin_memcpy(&x, &raw, 16);
+            __builtin_memcpy(&x, &raw[u], 16);
             if (which == 0) {
                 if (a.act != kNone) {
-                    const u32x4 rz = piece_at<T>((const T*)a.z + r * a.ldz + c, some);
                     Vec<T, V> z;
-                    __builtin_memcpy(&z, &rz, 16);
+                    __builtin_memcpy(&z, &rz[u], 16);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         const float d = i < some ? (float)x.v[i] * slope<sizeof(T) == 4>((float)z.v[i], a.act) : 0.0f;
@@ -782,35 +868,9 @@ __global__ __launch_bounds__(256) void k_turn(Turns a)
     }
 }
 
-// dbias from the column sums per 64 rows: 64 columns a workgroup, four parts of
-// the tiles joined in order.
-template <typename T>
-__global__ __launch_bounds__(256) void k_dbias(const float* __restrict__ sums, int64_t tiles, int64_t cols,
-                                               T* __restrict__ dbias)
-{
-    __shared__ float part[4][64];
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + x, each = (tiles + 3) / 4;
-    const int64_t from = y * each, to = from + each < tiles ? from + each : tiles;
-    float sum = 0.0f;
-    if (c < cols)
-        for (int64_t t0 = from; t0 < to; t0 += 8) {
-            float v[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                v[u] = t0 + u < to ? sums[(t0 + u) * cols + c] : 0.0f;
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                sum += v[u];
-        }
-    part[y][x] = sum;
-    __syncthreads();
-    if (y == 0 && c < cols)
-        dbias[c] = T(((part[0][x] + part[1][x]) + part[2][x]) + part[3][x]);
-}
-
 // ------------------------------------------------------------------- host
 constexpr uint32_t kMostWgs = 1 << 22;
+constexpr int64_t kCus = 256; // of an MI355X
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
 
@@ -832,37 +892,76 @@ struct Shape {
     int64_t groups; // workgroups
 };
 
-Shape shape_of(int64_t rows, int64_t cols, int64_t depth, int dtype)
+// The tile for `n` products of one launch.
+int tile_for(const int64_t* rows, const int64_t* cols, const int64_t* stages, int n, int dtype)
 {
-    const int64_t stages = up(depth * (int64_t)elem_bytes(dtype), kRow);
-    Shape s{0, 1, (int)std::max<int64_t>(stages, 1), 0};
-    if (rows <= 16 || cols == 0)
-        return s;
-    const int64_t big = up(rows, 256) * up(cols, 256), mid = up(rows, 128) * up(cols, 128);
-    if (stages >= 8 && (double)up(big, 256) <= 0.625 * 0.5 * (double)up(mid, 256)) {
-        s.tile = 256;
-        s.groups = big;
-        return s;
+    int64_t big = 0, mid = 0, low = 0, least = stages[0];
+    for (int i = 0; i < n; ++i) {
+        big += up(rows[i], 256) * up(cols[i], 256);
+        mid += up(rows[i], 128) * up(cols[i], 128);
+        low += up(rows[i], 64) * up(cols[i], 128);
+        least = std::min(least, stages[i]);
     }
+    if (least >= 8 && (double)up(big, kCus) <= 0.625 * 0.5 * (double)up(mid, kCus))
+        return 256;
     // Tiles of 64 rows where they fill the last round better: one takes 0.55 of the other's time in binary32, 0.7 in
     // 16 bits (bound by what comes from L2), measured on 1000 x 5000 x 776 (88 us against 112; 21.6 against 20).
-    const int64_t low = up(rows, 64) * up(cols, 128);
-    s.tile = mid <= 128 || (dtype == kF32 ? 0.55 : 0.7) * (double)up(low, 256) < (double)up(mid, 256) ? 64 : 128;
-    const int64_t tiles = s.tile == 128 ? mid : low;
-    // a workgroup for every CU, each with at least 4 stages (binary32, whose products take four times as long: 2)
-    const int64_t want = std::min<int64_t>(256 / std::min<int64_t>(tiles, 256), stages / (dtype == kF32 ? 2 : 4));
-    if (want > 1) {
-        s.steps = (int)up(stages, want);
-        s.slices = (int)up(stages, s.steps);
+    return mid <= 128 || (dtype == kF32 ? 0.55 : 0.7) * (double)up(low, kCus) < (double)up(mid, kCus) ? 64 : 128;
+}
+
+int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return up(rows, tile) * up(cols, tile == 256 ? 256 : 128); }
+
+// How `n` products of one launch are cut: one tile for all, and slices of one
+// length, so that there is a workgroup for every CU (with at least 4 stages, or
+// 2 in binary32, whose products take four times as long).
+void shapes_of(const int64_t* rows, const int64_t* cols, const int64_t* depth, int n, int dtype, Shape* s)
+{
+    int64_t stages[2], most = 1, tiles = 0;
+    for (int i = 0; i < n; ++i) {
+        stages[i] = std::max<int64_t>(up(depth[i] * (int64_t)elem_bytes(dtype), kRow), 1);
+        most = std::max(most, stages[i]);
     }
-    s.groups = tiles * s.slices;
+    const int tile = tile_for(rows, cols, stages, n, dtype);
+    for (int i = 0; i < n; ++i)
+        tiles += tiles_of(rows[i], cols[i], tile);
+    int64_t steps = most;
+    if (tile != 256 && tiles < kCus)
+        for (int64_t slices = 2; slices <= kCus; ++slices) {
+            const int64_t len = up(most, slices);
+            int64_t wgs = 0;
+            for (int i = 0; i < n; ++i)
+                wgs += tiles_of(rows[i], cols[i], tile) * up(stages[i], len);
+            if (wgs > kCus || len < (dtype == kF32 ? 2 : 4))
+                break;
+            steps = len;
+        }
+    int64_t groups = 0;
+    for (int i = 0; i < n; ++i) {
+        s[i].tile = tile;
+        s[i].slices = (int)up(stages[i], steps);
+        s[i].steps = (int)std::min(steps, stages[i]);
+        groups += tiles_of(rows[i], cols[i], tile) * s[i].slices;
+    }
+    for (int i = 0; i < n; ++i)
+        s[i].groups = groups;
+}
+
+Shape shape_of(int64_t rows, int64_t cols, int64_t depth, int dtype)
+{
+    Shape s{0, 1, 1, 0};
+    if (rows > 16 && cols > 0)
+        shapes_of(&rows, &cols, &depth, 1, dtype, &s);
     return s;
+}
+
+size_t sums_bytes(const Shape& s, int64_t rows, int64_t cols)
+{
+    return s.slices > 1 ? round256(sizeof(float) * (size_t)s.slices * (size_t)rows * (size_t)cols) : 0;
 }
 
 size_t part_bytes(int64_t rows, int64_t cols, int64_t depth, int dtype)
 {
-    const Shape s = shape_of(rows, cols, depth, dtype);
-    return s.slices > 1 ? round256(sizeof(float) * (size_t)s.slices * (size_t)rows * (size_t)cols) : 0;
+    return sums_bytes(shape_of(rows, cols, depth, dtype), rows, cols);
 }
 
 // 256 rows are addressed by 31 bits from the first.
@@ -873,16 +972,71 @@ bool rows_aligned(const void* p, int64_t ld, int dtype)
     return ((uintptr_t)p & 15) == 0 && ld * (int64_t)elem_bytes(dtype) % 16 == 0;
 }
 
+// Launches the products of p (the second one if its rows are set), and `sums`
+// workgroups for the column sums.
 template <typename T, int BM, int BN, int WM, int WN, bool DIRECT, int NB>
-hipError_t gemm_launch(GemmArgs g, const Epilogue& e, int slices, hipStream_t st)
+hipError_t gemm_launch(Products p, const Shape* s, int n, uint32_t sums, hipStream_t st)
 {
-    g.tiles_m = (uint32_t)up(g.rows, BM);
-    g.tiles_n = (uint32_t)up(g.cols, BN);
-    const uint32_t all = g.tiles_m * g.tiles_n;
-    for (g.tile0 = 0; g.tile0 < all; g.tile0 += kMostWgs) // a multiple of 8: the XCDs' turn goes on
-        hipLaunchKernelGGL((k_gemm<T, BM, BN, WM, WN, DIRECT, NB>), dim3(std::min(kMostWgs, all - g.tile0), slices),
-                           dim3((BM / WM) * (BN / WN) * 64), 0, st, g, e);
+    uint32_t ids[2] = {0, 0};
+    for (int i = 0; i < n; ++i) {
+        p.g[i].tiles_m = (uint32_t)up(p.g[i].rows, BM);
+        p.g[i].tiles_n = (uint32_t)up(p.g[i].cols, BN);
+        ids[i] = (uint32_t)up(p.g[i].tiles_m * p.g[i].tiles_n, 8) * 8 * (uint32_t)s[i].slices;
+    }
+    p.second = n > 1 ? ids[0] : kNoWork;
+    p.sums = sums ? ids[0] + ids[1] : kNoWork;
+    const uint32_t all = ids[0] + ids[1] + sums;
+    // (a part of a long launch begins with a whole turn of the XCDs; two products together are never that long)
+    for (p.g[0].tile0 = 0; p.g[0].tile0 < all; p.g[0].tile0 += kMostWgs)
+        hipLaunchKernelGGL((k_gemm<T, BM, BN, WM, WN, DIRECT, NB>), dim3(std::min(kMostWgs, all - p.g[0].tile0)),
+                           dim3((BM / WM) * (BN / WN) * 64), 0, st, p);
     return hipGetLastError();
+}
+
+template <typename T>
+hipError_t gemm_tiled(const Products& p, const Shape* s, int n, bool direct, uint32_t sums, hipStream_t st)
+{
+    if (s->tile == 256 && direct)
+        return gemm_launch<T, 256, 256, 128, 64, true, 2>(p, s, n, sums, st);
+    if (s->tile >= 128 && direct && s->groups <= kCus)
+        return gemm_launch<T, 128, 128, 32, 64, true, 4>(p, s, n, sums, st);
+    if (s->tile >= 128 && direct)
+        return gemm_launch<T, 128, 128, 32, 64, true, 2>(p, s, n, sums, st);
+    if (s->tile >= 128)
+        return gemm_launch<T, 128, 128, 32, 64, false, 2>(p, s, n, sums, st);
+    if (direct)
+        return gemm_launch<T, 64, 128, 16, 64, true, 3>(p, s, n, sums, st);
+    return gemm_launch<T, 64, 128, 32, 64, false, 2>(p, s, n, sums, st);
+}
+
+// The slices of those products that have several, joined.
+template <typename T>
+hipError_t join(const Products& p, const Shape* s, int n, hipStream_t st)
+{
+    Join j{};
+    uint32_t wgs[2] = {0, 0};
+    int m = 0;
+    for (int i = 0; i < n; ++i)
+        if (s[i].slices > 1) {
+            j.part[m] = p.g[i].part;
+            j.slices[m] = s[i].slices;
+            j.rows[m] = p.g[i].rows;
+            j.cols[m] = p.g[i].cols;
+            j.e[m] = p.e[i];
+            wgs[m] = (uint32_t)std::min<int64_t>(up(p.g[i].rows * up(p.g[i].cols, 4), 256), kMostWgs / 2);
+            ++m;
+        }
+    if (!m)
+        return hipSuccess;
+    j.second = m > 1 ? wgs[0] : kNoWork;
+    hipLaunchKernelGGL((k_gemm_join<T>), dim3(wgs[0] + wgs[1]), dim3(256), 0, st, j);
+    return hipGetLastError();
+}
+
+bool can_direct(const GemmArgs& g, int dtype)
+{
+    return rows_aligned(g.A, g.lda, dtype) && rows_aligned(g.B, g.ldb, dtype) &&
+           g.depth * (int64_t)elem_bytes(dtype) % 16 == 0 && near(std::max(g.lda, g.ldb), dtype);
 }
 
 // C = A B^T with its epilogue; `part` holds part_bytes.
@@ -904,27 +1058,11 @@ hipError_t gemm(GemmArgs g, const Epilogue& e, int dtype, void* part, hipStream_
             hipLaunchKernelGGL((k_gemm_few<T, 1>), dim3((unsigned)wgs), dim3(256), 0, st, g, e);
         return hipGetLastError();
     }
-    const bool direct = rows_aligned(g.A, g.lda, dtype) && rows_aligned(g.B, g.ldb, dtype) &&
-                        g.depth * (int64_t)sizeof(T) % 16 == 0 && near(std::max(g.lda, g.ldb), dtype);
-    hipError_t err;
-    if (s.tile == 256 && direct)
-        err = gemm_launch<T, 256, 256, 128, 64, true, 2>(g, e, 1, st);
-    else if (s.tile >= 128 && direct && s.groups <= 256)
-        err = gemm_launch<T, 128, 128, 32, 64, true, 4>(g, e, s.slices, st);
-    else if (s.tile >= 128 && direct)
-        err = gemm_launch<T, 128, 128, 32, 64, true, 2>(g, e, s.slices, st);
-    else if (s.tile >= 128)
-        err = gemm_launch<T, 128, 128, 32, 64, false, 2>(g, e, s.slices, st);
-    else if (direct)
-        err = gemm_launch<T, 64, 128, 16, 64, true, 3>(g, e, s.slices, st);
-    else
-        err = gemm_launch<T, 64, 128, 32, 64, false, 2>(g, e, s.slices, st);
-    if (err != hipSuccess || s.slices == 1)
-        return err;
-    const int64_t wgs = std::min<int64_t>(up(g.rows * up(g.cols, 4), 256), kMostWgs);
-    hipLaunchKernelGGL((k_gemm_join<T>), dim3((unsigned)wgs), dim3(256), 0, st, (const float*)part, s.slices, g.rows,
-                       g.cols, e);
-    return hipGetLastError();
+    Products p{};
+    p.g[0] = g;
+    p.e[0] = e;
+    const hipError_t err = gemm_tiled<T>(p, &s, 1, can_direct(g, dtype), 0, st);
+    return err == hipSuccess ? join<T>(p, &s, 1, st) : err;
 }
 
 template <typename T>
@@ -941,6 +1079,15 @@ struct GradWork {
     int64_t Mp, Np; // rows of whole pieces
     size_t bytes;
 };
+
+// Whether dX and dW can share a launch (those of few rows have a kernel of their own).
+bool together(int64_t M, int64_t N, int64_t K) { return M > 16 && N > 16 && K > 0; }
+
+void grad_shapes(int64_t M, int64_t N, int64_t K, int dtype, Shape* s)
+{
+    const int64_t rows[2] = {M, N}, cols[2] = {K, K}, depth[2] = {N, M};
+    shapes_of(rows, cols, depth, 2, dtype, s);
+}
 
 GradWork grad_work(int64_t M, int64_t N, int64_t K, int dtype, void* base)
 {
@@ -960,7 +1107,13 @@ GradWork grad_work(int64_t M, int64_t N, int64_t K, int dtype, void* base)
     w.x_t = take(es * (size_t)K * (size_t)w.Mp);
     w.w_t = take(es * (size_t)K * (size_t)w.Np);
     w.sums = take(sizeof(float) * (size_t)up(M, 64) * (size_t)N);
-    w.part = take(std::max(part_bytes(M, K, N, dtype), part_bytes(N, K, M, dtype)));
+    size_t part = std::max(part_bytes(M, K, N, dtype), part_bytes(N, K, M, dtype));
+    if (together(M, N, K)) {
+        Shape s[2];
+        grad_shapes(M, N, K, dtype, s);
+        part = std::max(part, sums_bytes(s[0], M, K) + sums_bytes(s[1], N, K));
+    }
+    w.part = take(part);
     w.bytes = at;
     return w;
 }
@@ -984,27 +1137,46 @@ hipError_t grad_typed(const LinearGradLaunch& a, hipStream_t st)
     t.sums = a.dbias ? (float*)w.sums : nullptr;
     if (!t.job[0].turned && !t.dz && !t.sums)
         t.job[0].tiles = 0;
-    t.tiles = t.job[0].tiles + t.job[1].tiles + t.job[2].tiles;
+    t.tiles = t.job[0].tiles + t.job[1].tiles + t.job[2].tiles; // (64 x 64 elements each: below 2^32 in any memory)
     if (t.tiles)
-        hipLaunchKernelGGL((k_turn<T>), dim3((unsigned)std::min<int64_t>(t.tiles, kMostWgs)), dim3(256), 0, st, t);
+        hipLaunchKernelGGL((k_turn<T>), dim3((unsigned)std::min<int64_t>(t.tiles, kMostWgs)),
+                           dim3(kTurnThreads), 0, st, t);
     hipError_t err = hipGetLastError();
-    if (a.dx && err == hipSuccess) {
-        GemmArgs g{as_is ? a.dy : w.dz, w.w_t, as_is ? a.lddy : w.Np, w.Np, a.M, a.K, a.N, 0, 0, 0, 0, nullptr};
-        if (!as_is)
-            g.depth = w.Np; // the zeros behind a row are part of it: whole pieces
-        const Epilogue e{nullptr, nullptr, a.dx, nullptr, 0, a.lddx, 0, a.M, a.K, kNone,
-                         near(a.lddx, a.dtype)};
-        err = gemm<T>(g, e, a.dtype, w.part, st);
+    if (err != hipSuccess)
+        return err;
+    // (where dZ lies in the workspace the zeros behind a row are part of it: whole pieces)
+    Products p{};
+    p.g[0] = GemmArgs{as_is ? a.dy : w.dz, w.w_t, as_is ? a.lddy : w.Np, w.Np, a.M, a.K, as_is ? a.N : w.Np, 0, 0, 0, 0,
+                      nullptr};
+    p.e[0] = Epilogue{nullptr, nullptr, a.dx, nullptr, 0, a.lddx, 0, a.M, a.K, kNone, near(a.lddx, a.dtype)};
+    p.g[1] = GemmArgs{w.dz_t, w.x_t, w.Mp, w.Mp, a.N, a.K, w.Mp, 0, 0, 0, 0, nullptr};
+    p.e[1] = Epilogue{nullptr, nullptr, a.dw, nullptr, 0, a.lddw, 0, a.N, a.K, kNone, near(a.lddw, a.dtype)};
+    p.col_sums = (const float*)w.sums;
+    p.row_tiles = up(a.M, 64);
+    p.cols = a.N;
+    p.dbias = a.dbias;
+    const uint32_t sums = a.dbias ? (uint32_t)up(a.N, 64) : 0;
+    Shape s[2];
+    const bool both = a.dx && a.dw && together(a.M, a.N, a.K) && can_direct(p.g[0], a.dtype) && can_direct(p.g[1], a.dtype);
+    if (both)
+        grad_shapes(a.M, a.N, a.K, a.dtype, s);
+    if (both && s->groups + sums < kMostWgs / 2) {
+        // both products and the column sums in one launch: the one fills what the other leaves idle
+        size_t at = 0;
+        for (int i = 0; i < 2; ++i) {
+            p.g[i].steps = s[i].steps;
+            p.g[i].part = s[i].slices > 1 ? (float*)((char*)w.part + at) : nullptr;
+            at += sums_bytes(s[i], p.g[i].rows, p.g[i].cols);
+        }
+        err = gemm_tiled<T>(p, s, 2, true, sums, st);
+        return err == hipSuccess ? join<T>(p, s, 2, st) : err;
     }
-    if (a.dw && err == hipSuccess) {
-        GemmArgs g{w.dz_t, w.x_t, w.Mp, w.Mp, a.N, a.K, w.Mp, 0, 0, 0, 0, nullptr};
-        const Epilogue e{nullptr, nullptr, a.dw, nullptr, 0, a.lddw, 0, a.N, a.K, kNone,
-                         near(a.lddw, a.dtype)};
-        err = gemm<T>(g, e, a.dtype, w.part, st);
-    }
-    if (a.dbias && a.N && err == hipSuccess) {
-        hipLaunchKernelGGL((k_dbias<T>), dim3((unsigned)up(a.N, 64)), dim3(256), 0, st, (const float*)w.sums,
-                           up(a.M, 64), a.N, (T*)a.dbias);
+    if (a.dx)
+        err = gemm<T>(p.g[0], p.e[0], a.dtype, w.part, st);
+    if (a.dw && err == hipSuccess)
+        err = gemm<T>(p.g[1], p.e[1], a.dtype, w.part, st);
+    if (sums && err == hipSuccess) {
+        hipLaunchKernelGGL((k_dbias<T>), dim3(sums), dim3(512), 0, st, p);
         err = hipGetLastError();
     }
     return err;

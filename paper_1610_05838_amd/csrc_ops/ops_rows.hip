@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int64_t kMostWgs = 1 << 22; // of a launch; workgroups then take several parts
+constexpr int64_t kInfinityCache = 256 << 20;
 
 // ---------------------------------------------------------------- lookup
 //
@@ -27,7 +28,11 @@ constexpr int64_t kMostWgs = 1 << 22; // of a launch; workgroups then take sever
 // thread has kAhead rows' loads in flight: the ids first, then the rows.
 constexpr int kAhead = 4;
 
-template <typename T, int V>
+//
+// ONCE: past the caches, where `out` is larger than the Infinity Cache and its
+// rows are whole cache lines (1.4 M rows of 512 bytes: 202 us, 4.2 TB/s, against
+// 225; 41 MB that stay in the caches: 11.7 us against 10.4).
+template <typename T, int V, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_rows_get(const T* __restrict__ table, int64_t rows, int64_t ld, int k,
                                                        const int32_t* __restrict__ ids, int64_t ids_stride,
                                                        int64_t count, float scale, T* __restrict__ out,
@@ -64,8 +69,12 @@ __global__ __launch_bounds__(kThreads) void k_rows_get(const T* __restrict__ tab
 #pragma unroll
                 for (int e = 0; e < V; ++e)
                     x[u].v[e] = T((float)x[u].v[e] * scale);
-                if (f0 + u * kThreads < total)
-                    store_vec<T, V>(out + (row0 + row[u]) * ld_out + col[u], x[u]);
+                if (f0 + u * kThreads < total) {
+                    if (ONCE)
+                        store_once<T, V>(out + (row0 + row[u]) * ld_out + col[u], x[u]);
+                    else
+                        store_vec<T, V>(out + (row0 + row[u]) * ld_out + col[u], x[u]);
+                }
             }
         }
     }
@@ -77,9 +86,12 @@ hipError_t get_launch(const RowsLaunch& a, hipStream_t st)
     const int nv = (a.k + V - 1) / V;
     const int per_wg = std::max(1, kThreads * kAhead / nv);
     const int64_t wgs = std::min((a.count + per_wg - 1) / per_wg, kMostWgs);
-    hipLaunchKernelGGL((k_rows_get<T, V>), dim3((unsigned)wgs), dim3(kThreads), 0, st, (const T*)a.table, a.rows, a.ld,
-                       a.k, a.ids, a.ids_stride, a.count, a.scale, (T*)a.out, a.ld_out, per_wg,
-                       fast_div((uint32_t)nv));
+    const int64_t row = (int64_t)a.k * (int64_t)sizeof(T), pitch = a.ld_out * (int64_t)sizeof(T);
+    const bool once = V * sizeof(T) == 16 && ((uintptr_t)a.out & 127) == 0 && row % 128 == 0 && pitch % 128 == 0 &&
+                      a.count * row > kInfinityCache;
+    hipLaunchKernelGGL((once ? k_rows_get<T, V, V * sizeof(T) == 16> : k_rows_get<T, V, false>), dim3((unsigned)wgs),
+                       dim3(kThreads), 0, st, (const T*)a.table, a.rows, a.ld, a.k, a.ids, a.ids_stride, a.count,
+                       a.scale, (T*)a.out, a.ld_out, per_wg, fast_div((uint32_t)nv));
     return hipGetLastError();
 }
 

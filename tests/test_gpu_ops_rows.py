@@ -65,6 +65,22 @@ def test_embed(dtype, k):
             assert torch.equal(M.embed(table, ids, scale=scale).double(), M.embed(table, ids.clone(), scale).double())
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
+def test_embed_larger_than_the_caches(dtype):
+    """A result of 300 MB: rows of whole cache lines, and the same rows one element off."""
+    k, rows = 256, 5000
+    count = 300 * 2**20 // (k * torch.finfo(dtype).bits // 8)
+    g = rng(2)
+    table = torch.randn(rows, k, generator=g, device="cuda").to(dtype)
+    ids = torch.randint(-1, rows, (count,), generator=g, device="cuda", dtype=torch.int32)
+    want = torch.where((ids >= 0)[:, None], table[ids.clamp(min=0).long()], torch.zeros_like(table[:1]))
+    assert torch.equal(M.embed(table, ids), want)
+    out, store = pitched(count, k, k, dtype, fill=7.0, shift=1)
+    M.embed(table, ids, out=out)
+    assert torch.equal(out, want)
+    assert float(store[0]) == 7.0 and bool((store[1 + count * k:] == 7.0).all())
+
+
 def test_embed_padding_reads_no_row():
     """Ids outside the table give zeros, whatever the table holds."""
     table = torch.full((4, 40), float("nan"), device="cuda")
