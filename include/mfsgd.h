@@ -512,8 +512,8 @@ enum { MFSGD_BF16 = 2 };
 /* Rows by id: out[i, 0..k) = scale * table[ids[i], 0..k) for i in [0, count).
  * ids[i] is read at ids + i * ids_stride, so a column of an mfsgd_sample array
  * (stride 3) is an id array.  An id outside [0, rows) stands for no row
- * (padding): its row of `out` is zero.  rows in [1, 2^31-1], k and ids_stride
- * at least 1, count at most 2^31-1. */
+ * (padding): its row of `out` is zero.  rows in [1, 2^31-1], k in [1, 2^22],
+ * ids_stride in [1, 2^28], count in [0, 2^31-1]. */
 int mfsgd_embed(const void* table, int64_t rows, int64_t ld, int32_t k, int32_t dtype, const int32_t* ids,
                 int64_t ids_stride, int64_t count, float scale, void* out, int64_t ld_out, void* stream);
 

@@ -56,6 +56,8 @@ bool matrix_ok(const void* p, int64_t rows, int64_t width, int64_t ld, int dtype
 
 bool dtype_ok(int32_t d) { return d == kF32 || d == kF16 || d == kBF16; }
 
+constexpr int32_t kMostColumns = 1 << 22; // 64 to 512 columns a workgroup, on the grid's second axis
+
 int check_work(const void* work, int64_t have, size_t need)
 {
     REQUIRE(need == 0 || (work && have >= 0 && (uint64_t)have >= need), "the workspace is too small");
@@ -75,7 +77,7 @@ int embed_impl(const RowsLaunch& a, void* stream)
 {
     REQUIRE(dtype_ok(a.dtype), "unknown dtype");
     REQUIRE(a.rows >= 1 && a.rows <= INT32_MAX, "rows must be in [1, 2^31-1]");
-    REQUIRE(a.k >= 1, "k must be at least 1");
+    REQUIRE(a.k >= 1 && a.k <= kMostColumns, "k must be in [1, 2^22]");
     if (int rc = check_ids(a.ids, a.ids_stride, a.count))
         return rc;
     REQUIRE(matrix_ok(a.table, a.rows, a.k, a.ld, a.dtype), "table is NULL or misaligned, or ld is below k");
@@ -87,7 +89,7 @@ int embed_grad_impl(RowsGradLaunch a, void* work, int64_t bytes, void* stream)
 {
     REQUIRE(dtype_ok(a.dtype), "unknown dtype");
     REQUIRE(a.rows >= 1 && a.rows <= INT32_MAX, "rows must be in [1, 2^31-1]");
-    REQUIRE(a.k >= 1, "k must be at least 1");
+    REQUIRE(a.k >= 1 && a.k <= kMostColumns, "k must be in [1, 2^22]");
     if (int rc = check_ids(a.ids, a.ids_stride, a.count))
         return rc;
     REQUIRE(matrix_ok(a.dout, a.count, a.k, a.ld_dout, a.dtype), "dout is NULL or misaligned, or ld_dout is below k");
@@ -303,7 +305,7 @@ int mfsgd_embed_grad_workspace(int64_t count, int32_t k, int64_t* bytes)
     return guarded([&]() -> int {
         REQUIRE(bytes, "NULL bytes");
         REQUIRE(count >= 0 && count <= INT32_MAX, "count must be in [0, 2^31-1]");
-        REQUIRE(k >= 1, "k must be at least 1");
+        REQUIRE(k >= 1 && k <= kMostColumns, "k must be in [1, 2^22]");
         *bytes = (int64_t)rows_grad_bytes(count, k);
         return MFSGD_OK;
     });

@@ -424,6 +424,10 @@ __global__ __launch_bounds__(kThreads) void k_sort_place(const uint32_t* __restr
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const uint32_t mask = (1u << bits) - 1;
     const int64_t base = (int64_t)blockIdx.x * CHUNK + wave * (steps * 64) + lane;
+    // all loads first: their latencies are most of this kernel
+    const bool used = threadIdx.x <= mask;
+    const uint32_t in_all = used ? totals[threadIdx.x] : 0;
+    const uint32_t in_earlier = used ? hist[(int64_t)threadIdx.x * gridDim.x + blockIdx.x] : 0;
 #pragma unroll
     for (int w = 0; w < 4; ++w)
         next[w][threadIdx.x] = 0;
@@ -443,9 +447,8 @@ __global__ __launch_bounds__(kThreads) void k_sort_place(const uint32_t* __restr
         if (base + s * 64 < count)
             atomicAdd(&next[wave][key[s] >> shift & mask], 1u);
     uint32_t total;
-    uint32_t at = block_scan(threadIdx.x <= mask ? totals[threadIdx.x] : 0, sums, total);
-    if (threadIdx.x <= mask) {
-        at += hist[(int64_t)threadIdx.x * gridDim.x + blockIdx.x];
+    uint32_t at = block_scan(in_all, sums, total) + in_earlier;
+    if (used) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const uint32_t n = next[w][threadIdx.x];
@@ -821,9 +824,11 @@ hipError_t zero_typed(const RowsGradLaunch& a, hipStream_t st)
     return v == 4 ? zero_launch<T, 4>(a, st) : v == 2 ? zero_launch<T, 2>(a, st) : zero_launch<T, 1>(a, st);
 }
 
-// Tokens of a tile: 64, or fewer where that leaves the chip without enough
-// wavefronts to cover the loads' latency.
-int tile_of(int64_t count) { return count >= 64 * 8192 ? 64 : count >= 32 * 8192 ? 32 : 16; }
+// Tokens of a tile: 64 (a lane each), or fewer (at least 16) where that leaves
+// the chip without 4096 wavefronts.  Half the tiles that it holds at once are as
+// fast as all of them, and long rows then have half as many parts to join
+// (262,144 Zipf tokens: 18 + 7 us with tiles of 64, 19 + 11 with tiles of 32).
+int tile_of(int64_t count) { return (int)std::min<int64_t>(64, std::max<int64_t>(16, (count + 4095) / 4096)); }
 
 // Tokens of a chunk of the sort: as few as still give every CU one (the sort's
 // kernels are bound by their chains of dependent steps), but not so many chunks

@@ -300,7 +300,8 @@ def debug_priority(s: int, stream=None):
 # --- operators on tables, gradients (see the header for what each computes) ---
 #
 # Outputs and workspaces not passed in are allocated on the stream the work runs
-# on.  Row-major matrices may have any row pitch; a tensor on another device
+# on; tensors given to a call on another stream than the current one may be
+# freed right after it (the order of work on the two is the caller's).  Row-major matrices may have any row pitch; a tensor on another device
 # than the current one, of another dtype than its call's or with strided
 # columns is refused before anything is enqueued.
 
@@ -321,6 +322,13 @@ class _On:
             if stream.device_index != self.device:
                 raise ValueError("the stream is on another device than the current one")
             self.handle = stream.cuda_stream
+
+    def uses(self, *tensors):
+        """Keeps the memory of tensors freed after this call until the work on a stream of the caller's is done."""
+        if self.stream is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
 
     def empty(self, shape, dtype):
         if self.stream is None:
@@ -372,10 +380,16 @@ def _ids(t, device):
     return t.data_ptr(), stride, n
 
 
-def _grad_workspace(on, count, k):
+@functools.lru_cache(maxsize=4096)
+def _bytes(fn, *sizes):
+    """What a ..._workspace call says of these sizes (it depends on nothing else)."""
     n = C.c_int64()
-    _check(lib().mfsgd_embed_grad_workspace(count, k, C.byref(n)), "mfsgd_embed_grad_workspace")
-    return on.workspace(n.value)
+    _check(getattr(lib(), fn)(*sizes, C.byref(n)), fn)
+    return n.value
+
+
+def _grad_workspace(on, count, k):
+    return on.workspace(_bytes("mfsgd_embed_grad_workspace", count, k))
 
 
 def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out=None, stream=None) -> torch.Tensor:
@@ -390,6 +404,7 @@ def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out=None, 
         ld_out = k
     else:
         ld_out = _matrix(out, "out", on.device, table.dtype, (count, k))
+    on.uses(table, ids, out)
     _check(lib().mfsgd_embed(table.data_ptr(), rows, ld, k, _DTYPES[table.dtype], idp, stride, count, scale,
                              out.data_ptr(), ld_out, on.handle), "mfsgd_embed")
     return out
@@ -414,6 +429,7 @@ def embed_grad(dout: torch.Tensor, ids: torch.Tensor, rows: int, scale: float = 
     else:
         ld_out = _matrix(out, "out", on.device, dout.dtype, (rows, k))
     work, nbytes, keep = _grad_workspace(on, count, k)
+    on.uses(dout, ids, out)
     _check(lib().mfsgd_embed_grad(dout.data_ptr(), ld, idp, stride, count, k, _DTYPES[dout.dtype], scale,
                                   out.data_ptr(), rows, ld_out, accumulate, work, nbytes, on.handle),
            "mfsgd_embed_grad")
@@ -432,6 +448,7 @@ def rows(side: int, ids: torch.Tensor, k: int, dtype=None, scale: float = 1.0, o
         ld_out = k
     else:
         ld_out = _matrix(out, "out", on.device, dtype, (count, k))
+    on.uses(ids, out)
     _check(lib().mfsgd_rows(side, idp, stride, count, k, _DTYPES[dtype], scale, out.data_ptr(), ld_out, on.handle),
            "mfsgd_rows")
     return out
@@ -448,6 +465,7 @@ def add_rows(side: int, dout: torch.Tensor, ids: torch.Tensor, scale: float, str
     if n != count:
         raise ValueError(f"dout has {n} rows for {count} ids")
     work, nbytes, keep = _grad_workspace(on, count, k)
+    on.uses(dout, ids)
     _check(lib().mfsgd_add_rows(side, dout.data_ptr(), ld, idp, stride, count, k, _DTYPES[dout.dtype], scale, work,
                                 nbytes, on.handle), "mfsgd_add_rows")
 
@@ -480,9 +498,8 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias=None, residual=None, act: str 
         ldy = _matrix(out, "out", on.device, dt, (M, N))
     z = on.empty((M, N), dt) if keep_z else None
     code = _DTYPES[dt]
-    n = C.c_int64()
-    _check(lib().mfsgd_linear_workspace(M, N, K, code, C.byref(n)), "mfsgd_linear_workspace")
-    work, nbytes, keep = on.workspace(n.value)
+    work, nbytes, keep = on.workspace(_bytes("mfsgd_linear_workspace", M, N, K, code))
+    on.uses(x, w, bias, residual, out)
     _check(lib().mfsgd_linear(x.data_ptr(), ldx, w.data_ptr(), ldw, bp,
                               None if residual is None else residual.data_ptr(), ldr, M, N, K, code, ACTS[act],
                               out.data_ptr(), ldy, z.data_ptr() if keep_z else None, max(N, 1), work, nbytes,
@@ -506,12 +523,11 @@ def linear_grad(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, z=None, act:
         raise ValueError("the gradient of an activation needs z")
     ldz = 0 if z is None else _matrix(z, "z", on.device, dt, (M, N))
     code = _DTYPES[dt]
-    n = C.c_int64()
-    _check(lib().mfsgd_linear_grad_workspace(M, N, K, code, C.byref(n)), "mfsgd_linear_grad_workspace")
-    work, nbytes, keep = on.workspace(n.value)
+    work, nbytes, keep = on.workspace(_bytes("mfsgd_linear_grad_workspace", M, N, K, code))
     gx = on.empty((M, K), dt) if dx else None
     gw = on.empty((N, K), dt) if dw else None
     gb = on.empty((N,), dt) if dbias else None
+    on.uses(dy, x, w, z)
     _check(lib().mfsgd_linear_grad(dy.data_ptr(), lddy, None if z is None else z.data_ptr(), ldz, x.data_ptr(), ldx,
                                    w.data_ptr(), ldw, M, N, K, code, ACTS[act], gx.data_ptr() if dx else None,
                                    max(K, 1), gw.data_ptr() if dw else None, max(K, 1),
@@ -535,6 +551,7 @@ def scores(users: torch.Tensor, n: int, dtype=None, bias=None, act: str = "none"
     need = C.c_int64()
     _check(lib().mfsgd_scores_workspace(count, C.byref(need)), "mfsgd_scores_workspace")
     work, nbytes, keep = on.workspace(need.value)
+    on.uses(users, bias, out)
     _check(lib().mfsgd_scores(up, stride, count, n, _DTYPES[dtype], bp, ACTS[act], out.data_ptr(), ld, work, nbytes,
                               on.handle), "mfsgd_scores")
     return out
@@ -561,9 +578,7 @@ class TensorList:
                 raise ValueError("the tensors must be on one device")
             self.entries[i].data, self.entries[i].n = t.data_ptr(), t.numel()
             self.entries[i].dtype = _DTYPES[t.dtype]
-        n = C.c_int64()
-        _check(lib().mfsgd_norm_workspace(len(self.tensors), C.byref(n)), "mfsgd_norm_workspace")
-        self.workspace_bytes = n.value
+        self.workspace_bytes = _bytes("mfsgd_norm_workspace", len(self.tensors))
 
     def __len__(self):
         return len(self.tensors)
@@ -573,6 +588,7 @@ def _tensor_list(tensors, on):
     a = tensors if isinstance(tensors, TensorList) else TensorList(tensors)
     if a.device is not None and a.device != on.device:
         raise ValueError("the tensors are on another device than the current one")
+    on.uses(*a.tensors)
     return a
 
 

@@ -226,6 +226,26 @@ def test_offsets_past_32_bits():
     assert int(torch.count_nonzero(table[::, 0])) == 4
 
 
+def test_tensors_freed_after_a_call_on_another_stream():
+    """What a call on a stream of the caller's reads may be freed at once: its memory is not handed out before."""
+    g = rng(6)
+    side = torch.cuda.Stream()
+    for count in (3000, 30_000):
+        dout = torch.randint(-4, 5, (count, 64), generator=g, device="cuda").float()
+        ids = make_ids("uniform", count, 100, g)
+        want = grad_want(dout, ids, 100, 1.0)
+        a, b = dout.clone(), ids.clone()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)  # the call's work begins later
+        got = M.embed_grad(a, b, 100, stream=side)
+        del a, b
+        junk = [torch.full((count, 64), 7.0, device="cuda"), torch.full((count,), 5, dtype=torch.int32, device="cuda")]
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(got.double(), want)
+        del junk
+
+
 def test_streams_and_graphs():
     """On another stream, and captured: every replay sees the inputs as they are then."""
     g = rng(9)

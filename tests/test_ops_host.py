@@ -42,7 +42,7 @@ GRAD = dict(dout=A, ld_dout=8, ids=A, ids_stride=1, count=4, k=8, dtype=0, scale
 @pytest.mark.parametrize("what", [
     dict(table=None), dict(table=A + 2), dict(rows=0), dict(rows=-1), dict(rows=2**31), dict(ld=7), dict(k=0),
     dict(k=-3), dict(dtype=3), dict(dtype=-1), dict(ids=None), dict(ids=A + 1), dict(ids_stride=0),
-    dict(ids_stride=-1), dict(count=-1), dict(count=2**31), dict(out=None), dict(out=A + 1), dict(ld_out=7),
+    dict(ids_stride=-1), dict(ids_stride=2**28 + 1), dict(k=2**22 + 1, ld=2**23, ld_out=2**23), dict(count=-1), dict(count=2**31), dict(out=None), dict(out=A + 1), dict(ld_out=7),
     dict(ld=BIG), dict(dtype=1, table=A + 1)])
 def test_embed_refuses(lib, what):
     refused(lib, "mfsgd_embed", changed(EMBED, **what))
@@ -50,7 +50,7 @@ def test_embed_refuses(lib, what):
 
 @pytest.mark.parametrize("what", [
     dict(dout=None), dict(dout=A + 2), dict(ld_dout=7), dict(ids=None), dict(ids=A + 2), dict(ids_stride=0),
-    dict(count=-1), dict(count=2**31), dict(k=0), dict(dtype=9), dict(dtable=None), dict(dtable=A + 1),
+    dict(count=-1), dict(count=2**31), dict(k=0), dict(k=2**22 + 1, ld=2**23, ld_dout=2**23), dict(dtype=9), dict(dtable=None), dict(dtable=A + 1),
     dict(rows=0), dict(rows=2**31), dict(ld=3),
     dict(count=100_000, work=None, nbytes=BIG), dict(count=100_000, work=A, nbytes=64),
     dict(count=100_000, work=A + 8, nbytes=BIG), dict(count=100_000, work=A, nbytes=-1)])
@@ -69,8 +69,8 @@ def test_embed_grad_workspace(lib):
     n = C.c_int64(-1)
     assert lib.mfsgd_embed_grad_workspace(10, 128, C.byref(n)) == 0 and n.value == 0
     assert lib.mfsgd_embed_grad_workspace(1_000_000, 128, C.byref(n)) == 0 and n.value >= 16_000_000
-    assert lib.mfsgd_embed_grad_workspace(INT32_MAX, 1 << 20, C.byref(n)) == 0 and n.value > 1 << 45
-    for count, k in ((-1, 8), (2**31, 8), (5, 0)):
+    assert lib.mfsgd_embed_grad_workspace(INT32_MAX, 1 << 22, C.byref(n)) == 0 and n.value > 1 << 45
+    for count, k in ((-1, 8), (2**31, 8), (5, 0), (5, 2**22 + 1)):
         refused(lib, "mfsgd_embed_grad_workspace", (count, k, C.byref(n)))
     refused(lib, "mfsgd_embed_grad_workspace", (5, 8, None))
 
