@@ -534,7 +534,9 @@ int mfsgd_embed_grad_workspace(int64_t count, int32_t k, int64_t* bytes);
  * rows), k and dtype must be the model's.
  * mfsgd_add_rows updates the factors in place as mfsgd_embed_grad does with
  * `accumulate` (workspace: mfsgd_embed_grad_workspace).  Ordered on `stream`
- * like an epoch.  ESTATE before mfsgd_init or on another device. */
+ * like an epoch; a captured graph holds the factors' addresses and must not be
+ * replayed after mfsgd_finalize or another mfsgd_init.  ESTATE before mfsgd_init
+ * or on another device. */
 enum { MFSGD_P = 0, MFSGD_Q = 1 };
 int mfsgd_rows(int32_t side, const int32_t* ids, int64_t ids_stride, int64_t count, int32_t k, int32_t dtype,
                float scale, void* out, int64_t ld_out, void* stream);
@@ -567,7 +569,7 @@ int mfsgd_linear_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, int64
  *   dZ = dY * act'(Z) elementwise,   dX = dZ W,   dW = dZ^T X,   dbias = column sums of dZ
  * (the residual's gradient is dY).  dx, dw and dbias may be NULL: left out; z may
  * be NULL for MFSGD_ACT_NONE; w may be NULL without dx, x without dw.  The slope
- * of relu at 0 is 0.  dZ is rounded to the dtype before the products (as the
+ * of relu at 0 is 0, of an act at NaN is NaN.  dZ is rounded to the dtype before the products (as the
  * matrix instructions take it) and summed unrounded into dbias. */
 int mfsgd_linear_grad(const void* dy, int64_t lddy, const void* z, int64_t ldz, const void* x, int64_t ldx,
                       const void* w, int64_t ldw, int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t act,
@@ -578,7 +580,8 @@ int mfsgd_linear_grad_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, 
 /* The model's answer: the scores of `count` users against all its items,
  *   out[i, v] = act(p_{users[i]} . q_v + bias[v])
  * (after mfsgd_init, on its device; k, n and dtype must be the model's).  bias (n
- * values) may be NULL.  A user outside [0, m) stands for none: act(bias). */
+ * values) may be NULL.  A user outside [0, m) stands for none, a row of zeros:
+ * act(bias). */
 int mfsgd_scores(const int32_t* users, int64_t users_stride, int64_t count, int64_t n, int32_t dtype,
                  const void* bias, int32_t act, void* out, int64_t ld_out, void* workspace, int64_t workspace_bytes,
                  void* stream);
@@ -589,10 +592,10 @@ int mfsgd_scores_workspace(int64_t count, int64_t* bytes); /* ESTATE before mfsg
  * the operators above, except that every tensor has a dtype of its own; `list`
  * is HOST memory, read before the call returns.
  *   norm = sqrt(sum over all tensors and elements of g^2)   (binary64)
- *   c    = norm <= max_norm ? 1 : max_norm / norm
- * A gradient that is not finite makes norm infinite or NaN and c 0 or NaN, as
- * the formula gives them (a NaN then reaches every element): the caller sees it
- * in *norm_dev.
+ *   c    = norm <= max_norm or max_norm infinite ? 1 : max_norm / norm
+ * A gradient that is not finite makes norm infinite or NaN and, under a finite
+ * max_norm, c 0 or NaN, as the formula gives them (a NaN then reaches every
+ * element): the caller sees it in *norm_dev.
  * Every call writes the norm to *norm_dev, one binary64 in caller-owned DEVICE
  * memory (0 for no elements). */
 typedef struct {

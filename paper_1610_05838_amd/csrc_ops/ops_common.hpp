@@ -51,6 +51,8 @@ __device__ __forceinline__ void store_vec(T* p, const Vec<T, E>& x)
     __builtin_memcpy(p, &x, sizeof(x));
 }
 
+constexpr int64_t kInfinityCache = 256 << 20; // bytes
+
 // Streams that are read or written once and are larger than the caches.
 template <typename T, int E>
 __device__ __forceinline__ Vec<T, E> load_once(const T* p)

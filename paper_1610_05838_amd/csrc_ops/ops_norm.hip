@@ -1,10 +1,12 @@
 // ops_norm.hip -- the global norm of many gradients, and what is done with it:
 //   norm = sqrt(sum over all tensors of g^2),
-//   c    = norm <= max_norm ? 1 : max_norm / norm,
+//   c    = norm <= max_norm or max_norm infinite ? 1 : max_norm / norm,
 //   clip g <- c g,  or  step p <- p - lr (c g + lambda p).
 //
 // Bound by memory: a norm reads g once; clipping reads it again and writes it; a
-// step reads g again and p and writes p.
+// step reads g again and p and writes p.  ONCE: gradients that are together
+// larger than the Infinity Cache are loaded past the caches, which have lost
+// their beginning by the time it is read again.
 //
 // Squares are summed in binary64 from the first: the square of a binary32 or
 // bfloat16 value leaves binary32's range at either end, a binary64 sum of such
@@ -64,7 +66,13 @@ __device__ __forceinline__ double block_sum(double x, double* sums)
     return x;
 }
 
-template <typename T>
+template <typename T, int V, bool ONCE>
+__device__ __forceinline__ Vec<T, V> load_some(const T* p)
+{
+    return ONCE ? load_once<T, V>(p) : load_vec<T, V>(p);
+}
+
+template <typename T, bool ONCE>
 __device__ __forceinline__ double squares(const T* __restrict__ g, int n, double sum)
 {
     constexpr int V = 16 / (int)sizeof(T), ahead = 4;
@@ -77,7 +85,7 @@ __device__ __forceinline__ double squares(const T* __restrict__ g, int n, double
         Vec<T, V> x[ahead];
 #pragma unroll
         for (int u = 0; u < ahead; ++u)
-            x[u] = load_vec<T, V>(g + (int64_t)(i0 + u * kThreads < whole ? i0 + u * kThreads : i0) * V);
+            x[u] = load_some<T, V, ONCE>(g + (int64_t)(i0 + u * kThreads < whole ? i0 + u * kThreads : i0) * V);
 #pragma unroll
         for (int u = 0; u < ahead; ++u)
             if (i0 + u * kThreads < whole) {
@@ -99,6 +107,7 @@ __device__ __forceinline__ double squares(const T* __restrict__ g, int n, double
     return sum;
 }
 
+template <bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_norm_part(Group a, double* __restrict__ part)
 {
     __shared__ double sums[4];
@@ -109,11 +118,11 @@ __global__ __launch_bounds__(kThreads) void k_norm_part(Group a, double* __restr
         const int64_t at = (int64_t)(chunk - a.first[t]) * kChunk;
         const int n = (int)(a.n[t] - at < kChunk ? a.n[t] - at : kChunk);
         if (a.dtype[t] == kF32)
-            sum = squares((const float*)a.g[t] + at, n, sum);
+            sum = squares<float, ONCE>((const float*)a.g[t] + at, n, sum);
         else if (a.dtype[t] == kF16)
-            sum = squares((const _Float16*)a.g[t] + at, n, sum);
+            sum = squares<_Float16, ONCE>((const _Float16*)a.g[t] + at, n, sum);
         else
-            sum = squares((const __bf16*)a.g[t] + at, n, sum);
+            sum = squares<__bf16, ONCE>((const __bf16*)a.g[t] + at, n, sum);
     }
     sum = block_sum(sum, sums);
     if (threadIdx.x == 0)
@@ -149,7 +158,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_fold(const double* __restrict
     }
 }
 
-template <typename T, bool STEP>
+template <typename T, bool STEP, bool ONCE>
 __device__ __forceinline__ void apply_to(T* p, const T* g, int n, float c, float lr, float lam)
 { // clipping: p is g
     constexpr int V = 16 / (int)sizeof(T), ahead = 4;
@@ -159,9 +168,9 @@ __device__ __forceinline__ void apply_to(T* p, const T* g, int n, float c, float
 #pragma unroll
         for (int u = 0; u < ahead; ++u) {
             const int i = i0 + u * kThreads < whole ? i0 + u * kThreads : i0;
-            x[u] = load_vec<T, V>(g + (int64_t)i * V);
+            x[u] = load_some<T, V, ONCE>(g + (int64_t)i * V);
             if (STEP)
-                y[u] = load_vec<T, V>(p + (int64_t)i * V);
+                y[u] = load_some<T, V, ONCE>(p + (int64_t)i * V);
         }
 #pragma unroll
         for (int u = 0; u < ahead; ++u) {
@@ -185,7 +194,7 @@ __device__ __forceinline__ void apply_to(T* p, const T* g, int n, float c, float
 
 // The clipping factor is rounded once, from binary64 to the binary32 that the
 // elements are computed in.
-template <bool STEP>
+template <bool STEP, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_norm_apply(Group a, const double* __restrict__ part, int64_t parts,
                                                          double max_norm, float lr, float lam,
                                                          double* __restrict__ norm_out)
@@ -194,8 +203,9 @@ __global__ __launch_bounds__(kThreads) void k_norm_apply(Group a, const double* 
     const double norm = sqrt(fold(part, parts, sums));
     if (norm_out && blockIdx.x == 0 && threadIdx.x == 0)
         *norm_out = norm;
-    const float c = norm <= max_norm ? 1.0f : (float)(max_norm / norm);
-    if (!STEP && norm <= max_norm)
+    const bool within = norm <= max_norm || isinf(max_norm); // a NaN is within no finite bound
+    const float c = within ? 1.0f : (float)(max_norm / norm);
+    if (!STEP && within)
         return; // c g = g
     int t = 0;
     for (uint32_t chunk = blockIdx.x; chunk < a.first[a.count]; chunk += gridDim.x) {
@@ -203,11 +213,11 @@ __global__ __launch_bounds__(kThreads) void k_norm_apply(Group a, const double* 
         const int64_t at = (int64_t)(chunk - a.first[t]) * kChunk;
         const int n = (int)(a.n[t] - at < kChunk ? a.n[t] - at : kChunk);
         if (a.dtype[t] == kF32)
-            apply_to<float, STEP>((float*)a.p[t] + at, (const float*)a.g[t] + at, n, c, lr, lam);
+            apply_to<float, STEP, ONCE>((float*)a.p[t] + at, (const float*)a.g[t] + at, n, c, lr, lam);
         else if (a.dtype[t] == kF16)
-            apply_to<_Float16, STEP>((_Float16*)a.p[t] + at, (const _Float16*)a.g[t] + at, n, c, lr, lam);
+            apply_to<_Float16, STEP, ONCE>((_Float16*)a.p[t] + at, (const _Float16*)a.g[t] + at, n, c, lr, lam);
         else
-            apply_to<__bf16, STEP>((__bf16*)a.p[t] + at, (const __bf16*)a.g[t] + at, n, c, lr, lam);
+            apply_to<__bf16, STEP, ONCE>((__bf16*)a.p[t] + at, (const __bf16*)a.g[t] + at, n, c, lr, lam);
     }
 }
 
@@ -251,13 +261,17 @@ hipError_t norm_apply(const NormTensor* list, int64_t count, int apply, double m
     double* part = (double*)work + 1;
     double* total = (double*)work;
     Group a;
+    int64_t bytes = 0;
+    for (int64_t i = 0; i < count; ++i)
+        bytes += list[i].n * (list[i].dtype == kF32 ? 4 : 2);
+    const bool once = bytes > kInfinityCache;
     int64_t parts = 0;
     for (int64_t i = 0; i < count;) {
         i = next_group(list, count, i, a);
         if (!a.count)
             break;
         const int64_t wgs = std::min<int64_t>(a.first[a.count], kMostWgs);
-        hipLaunchKernelGGL(k_norm_part, dim3((unsigned)wgs), dim3(kThreads), 0, st, a, part + parts);
+        hipLaunchKernelGGL((once ? k_norm_part<true> : k_norm_part<false>), dim3((unsigned)wgs), dim3(kThreads), 0, st, a, part + parts);
         parts += wgs;
     }
     const bool folded = !apply || parts > kFold || parts == 0;
@@ -277,10 +291,10 @@ hipError_t norm_apply(const NormTensor* list, int64_t count, int apply, double m
             break;
         const int64_t wgs = std::min<int64_t>(a.first[a.count], kMostWgs);
         if (apply == 2)
-            hipLaunchKernelGGL(k_norm_apply<true>, dim3((unsigned)wgs), dim3(kThreads), 0, st, a, part, parts,
+            hipLaunchKernelGGL((once ? k_norm_apply<true, true> : k_norm_apply<true, false>), dim3((unsigned)wgs), dim3(kThreads), 0, st, a, part, parts,
                                max_norm, lr, lam, norm);
         else
-            hipLaunchKernelGGL(k_norm_apply<false>, dim3((unsigned)wgs), dim3(kThreads), 0, st, a, part, parts,
+            hipLaunchKernelGGL((once ? k_norm_apply<false, true> : k_norm_apply<false, false>), dim3((unsigned)wgs), dim3(kThreads), 0, st, a, part, parts,
                                max_norm, lr, lam, norm);
         norm = nullptr; // written by the first
     }

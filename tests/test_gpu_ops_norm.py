@@ -133,6 +133,42 @@ def test_special_norms():
     assert float(M.clip_grads([t], math.inf)) == math.inf and float(t[4]) == 1.0  # inf <= inf: as they are
 
 
+def test_an_infinite_bound_clips_nothing():
+    for bad in (math.nan, math.inf):
+        t = torch.ones(100, device="cuda")
+        t[5] = bad
+        p = torch.ones(100, device="cuda")
+        norm = float(M.sgd_step([p], [t], 0.5))
+        assert math.isnan(norm) or norm == math.inf
+        assert not math.isfinite(float(p[5]))
+        p[5] = 0.5
+        assert bool((p == 0.5).all())
+        M.clip_grads([t], math.inf)
+        t[5] = 1.0
+        assert bool((t == 1.0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradients_larger_than_the_caches(dtype):
+    """More than 256 MB, in odd pieces that start off their alignment."""
+    each = 24_000_001 if dtype == F32 else 47_000_003
+    spec = [(each, dtype, 1), (257, F16, 3), (each, dtype, 3), (each + 7, dtype, 2)]
+    g, p = make(spec, 5), make(spec, 6, std=0.5)
+    old, grads = [t.clone() for t in p], [t.clone() for t in g]
+    want = norm64(g)
+    lr, lam, bound = float(np.float32(0.03)), float(np.float32(0.05)), 0.5
+    assert abs(float(M.grad_norm(g)) - want) <= 1e-12 * want
+    assert abs(float(M.sgd_step(p, g, lr, lam=lam, max_norm=bound * want)) - want) <= 1e-12 * want
+    for a, b, d in zip(old, p, g):
+        eps = torch.finfo(a.dtype).eps / 2
+        new = a.double() - lr * (bound * d.double() + lam * a.double())
+        mag = a.double().abs() + lr * (4 * bound * d.double().abs() + 3 * lam * a.double().abs()) + new.abs()
+        tol = mag * 2.0**-24 * 1.05 + new.abs() * eps * 1.01 + torch.finfo(a.dtype).smallest_normal * eps
+        assert bool(((b.double() - new).abs() <= tol).all())
+    M.clip_grads(g, want / 3)
+    check_clip(grads, g, 1 / 3)
+
+
 def test_one_tensor_twice_counts_twice():
     t = torch.full((50,), 2.0, device="cuda")
     assert abs(float(M.grad_norm([t, t])) - 20.0) < 1e-12
