@@ -83,7 +83,7 @@ __device__ __forceinline__ float slope(float z, int act)
 {
     switch (act) {
     case kRelu:
-        return z > 0.0f ? 1.0f : 0.0f;
+        return z > 0.0f ? 1.0f : z != z ? z : 0.0f; // a NaN stays one, as in the result
     case kSigmoid: {
         const float s = sigmoid<EXACT>(z);
         return s * (1.0f - s);
@@ -389,16 +389,16 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(Products p)
     const char* base[2] = {(const char*)((const T*)g.A + m0 * g.lda + k0), (const char*)((const T*)g.B + n0 * g.ldb + k0)};
     typedef typename Pick<DIRECT, uint32_t, uint64_t>::type Offset;
     Offset off[groups]; // from the tile's first row
+    const int last_m = g.rows - m0 < BM ? (int)(g.rows - m0) - 1 : BM - 1;
+    const int last_n = g.cols - n0 < BN ? (int)(g.cols - n0) - 1 : BN - 1;
 #pragma unroll
     for (int u = 0; u < groups; ++u) {
         const int group = wave * groups + u, row = group * copied + lane / pieces;
         if (group < BM / copied) {
-            const int64_t m = m0 + row < g.rows ? row : g.rows - 1 - m0;
-            off[u] = (Offset)((m * g.lda + pc * piece) * (int64_t)sizeof(T));
+            off[u] = ((Offset)(row < last_m ? row : last_m) * (Offset)g.lda + pc * piece) * (Offset)sizeof(T);
         } else {
-            const int r = row - BM, n = column_of<T>(r);
-            const int64_t col = n0 + n < g.cols ? n : g.cols - 1 - n0;
-            off[u] = (Offset)((col * g.ldb + pc * piece) * (int64_t)sizeof(T));
+            const int n = column_of<T>(row - BM);
+            off[u] = ((Offset)(n < last_n ? n : last_n) * (Offset)g.ldb + pc * piece) * (Offset)sizeof(T);
         }
     }
     // stages before `whole` lie inside the depth; in the last one pieces past it are zeros
@@ -682,7 +682,11 @@ __global__ __launch_bounds__(256) void k_gemm_join(Join p)
 }
 
 // Up to 16 rows (a batch of queries, a single token): bound by reading B, which
-// goes from memory to the matrix instructions' registers without a stop in LDS.
+// goes from memory to the matrix instructions' registers without a stop in LDS
+// (one row against 4096 x 4096 bfloat16 in the caches: 8.2 us, 4.1 TB/s; with the
+// tiles above 10.3), and by the latency of a launch and one trip to memory where B
+// is small (17,770 x 128 binary16: 4.1 us, the tiles 5.1; 512 x 512 binary32, 16
+// rows: 4.9 and 9.1).
 // A wavefront takes 16 columns; KW of a workgroup's 4 wavefronts share one such
 // tile, each a part of the depth, their sums joined in order.  Any alignment.
 // Rows and columns past the end repeat one that exists; their sums are not
@@ -912,8 +916,13 @@ int tile_for(const int64_t* rows, const int64_t* cols, const int64_t* stages, in
 int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return up(rows, tile) * up(cols, tile == 256 ? 256 : 128); }
 
 // How `n` products of one launch are cut: one tile for all, and slices of one
-// length, so that there is a workgroup for every CU (with at least 4 stages, or
-// 2 in binary32, whose products take four times as long).
+// length, so that there is a workgroup for every CU.  A stage takes 0.34 us (1.35
+// in binary32, whose products take four times as long), writing, reading and
+// joining the sums some 4: slices are of at least 8 stages (2; 512 x 512 x 2048
+// binary16: 12.1 us against 13.7 with 4), and there are several only where that
+// shortens a workgroup by more than the join takes (64 x 4096 x 1024 bfloat16: 8.8
+// us as one, 10.9 as two; 128 x 512 x 4096: 21.6 as one, 11.3 as eight; 333 x 500 x
+// 1001 binary32: 43 and 16).
 void shapes_of(const int64_t* rows, const int64_t* cols, const int64_t* depth, int n, int dtype, Shape* s)
 {
     int64_t stages[2], most = 1, tiles = 0;
@@ -931,10 +940,12 @@ void shapes_of(const int64_t* rows, const int64_t* cols, const int64_t* depth, i
             int64_t wgs = 0;
             for (int i = 0; i < n; ++i)
                 wgs += tiles_of(rows[i], cols[i], tile) * up(stages[i], len);
-            if (wgs > kCus || len < (dtype == kF32 ? 2 : 4))
+            if (wgs > kCus || len < (dtype == kF32 ? 2 : 8))
                 break;
             steps = len;
         }
+    if (most - steps < (dtype == kF32 ? 3 : 12))
+        steps = most;
     int64_t groups = 0;
     for (int i = 0; i < n; ++i) {
         s[i].tile = tile;
@@ -1049,8 +1060,9 @@ hipError_t gemm(GemmArgs g, const Epilogue& e, int dtype, void* part, hipStream_
     g.steps = s.steps;
     g.part = s.slices > 1 ? (float*)part : nullptr;
     if (s.tile == 0) {
-        // long rows: all four wavefronts on one tile
-        const bool shared = g.depth * (int64_t)sizeof(T) >= 1024;
+        // long rows: all four wavefronts on one tile (17,770 columns of 128 binary16: 4.1 us apart, 4.6 together; of
+        // 256: 5.1 and 4.6; 4096 of 4096: 21.5 and 8.2)
+        const bool shared = g.depth * (int64_t)sizeof(T) >= 512;
         const int64_t wgs = std::min<int64_t>(up(g.cols, shared ? 16 : 64), kMostWgs);
         if (shared)
             hipLaunchKernelGGL((k_gemm_few<T, 4>), dim3((unsigned)wgs), dim3(256), 0, st, g, e);

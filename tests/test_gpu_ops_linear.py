@@ -43,8 +43,8 @@ def act64(z, act):
 
 
 # few rows; tiles of 64, 128 and 256 rows; one slice of the depth and several; whole and ragged pieces
-SHAPES = [(0, 5, 3), (5, 0, 3), (1, 1, 1), (1, 17, 0), (40, 9, 0), (3, 1000, 7), (16, 65, 64), (16, 333, 1500), (2, 50, 4096),
-          (17, 16, 8), (64, 300, 100), (33, 129, 2048), (64, 5000, 65), (65, 64, 31), (128, 128, 64), (130, 257, 72),
+SHAPES = [(0, 5, 3), (5, 0, 3), (1, 1, 1), (1, 17, 0), (40, 9, 0), (3, 1000, 7), (16, 65, 64), (16, 333, 1500), (2, 50, 4096), (14, 51, 2619),
+          (16, 9000, 2050), (17, 16, 8), (64, 300, 100), (33, 129, 2048), (64, 5000, 65), (65, 64, 31), (128, 128, 64), (130, 257, 72),
           (300, 40, 511), (1000, 333, 500), (257, 4100, 1), (700, 3000, 40), (128, 128, 4096), (4000, 3500, 520)]
 
 
@@ -102,6 +102,17 @@ def test_special_values():
                 assert bool(torch.isnan(y[1]).all()) and bool((y[2] == (-math.inf if act == "none" else 0.0)).all())
                 assert bool((y[0] == k).all()) and bool((y[3:] == k).all())
             assert bool((M.linear(x, w, act="sigmoid")[2] == 0.0).all())
+
+
+def test_a_nan_before_the_activation_reaches_its_gradient():
+    for dtype in DTYPES:
+        x, w = torch.ones(40, 8, device="cuda", dtype=dtype), torch.ones(24, 8, device="cuda", dtype=dtype)
+        z = torch.ones(40, 24, device="cuda", dtype=dtype)
+        z[3, 5] = math.nan
+        for act in ACTS[1:]:
+            dx, dw, db = M.linear_grad(torch.ones_like(z), x, w, z=z, act=act)
+            assert bool(torch.isnan(dx[3]).all()) and bool(torch.isnan(dw[5]).all()) and math.isnan(float(db[5]))
+            assert int(torch.isnan(dx).sum()) == 8 and int(torch.isnan(dw).sum()) == 8 and int(torch.isnan(db).sum()) == 1
 
 
 def test_large_arguments():
