@@ -191,6 +191,12 @@ __device__ __forceinline__ void finish(const Epilogue& e, int64_t m, int64_t n, 
 //
 // B is the matrix instruction's row operand: a lane then holds 4 consecutive
 // columns of C per tile (see column_of).
+//
+// Bound by the matrix instructions and what feeds them from LDS: 4096^3 bfloat16
+// with bias, gelu, residual and Z kept 116-129 us, 1.1-1.2 PFLOP/s; by the epilogue
+// where the depth is short: 2048 x 39,780 x 128 binary16 with bias and sigmoid 61
+// us, 163 MB written at 2.7 TB/s (an exponential and a reciprocal per element are 17
+// us of the vector units, the rest of the epilogue as much again).
 constexpr int kRow = 128; // bytes of depth of a stage
 
 __device__ __attribute__((aligned(16))) const uint32_t g_zeros[4] = {0, 0, 0, 0};
@@ -198,13 +204,13 @@ __device__ __attribute__((aligned(16))) const uint32_t g_zeros[4] = {0, 0, 0, 0}
 struct GemmArgs {
     const void *A, *B;
     int64_t lda, ldb, rows, cols, depth;
-    uint32_t tiles_m, tiles_n, tile0; // of the whole product; this launch's first
+    uint32_t tiles_m, tiles_n, all, tile0; // of the whole product; with its slices; this launch's first
     int steps;                        // stages of one workgroup: a slice of the depth
     float* part;                      // the slices' sums [slice][rows][cols], or nullptr: one slice, finished here
 };
 
-// One launch's work: a product's tiles, slice by slice, the ids of a slice
-// rounded up to whole turns of the XCDs; from id `second` on another product's;
+// One launch's work: a product's tiles, slice by slice, the ids rounded up to
+// whole turns of the XCDs; from id `second` on another product's;
 // from id `sums` on the column sums of dZ (see k_turn).
 struct Products {
     GemmArgs g[2];
@@ -272,12 +278,14 @@ __device__ __forceinline__ int column_of(int r)
 }
 
 // Workgroups are dealt to the 8 XCDs in turn: each XCD takes a run of
-// consecutive tiles, and runs go down 8 tiles of rows before the next column, so
-// that the tiles of an XCD share rows of A and B in its L2.
-__device__ __forceinline__ void tile_place(const GemmArgs& g, uint32_t id, uint32_t& tm, uint32_t& tn)
+// consecutive tiles, slice by slice, and runs go down 8 tiles of rows before the
+// next column, so that the tiles of an XCD share rows of A and B in its L2.
+__device__ __forceinline__ void tile_place(const GemmArgs& g, uint32_t id, uint32_t& slice, uint32_t& tm, uint32_t& tn)
 {
-    const uint32_t all = g.tiles_m * g.tiles_n, x = id & 7;
-    const uint32_t t = x * (all >> 3) + (x < (all & 7) ? x : all & 7) + (id >> 3);
+    const uint32_t tiles = g.tiles_m * g.tiles_n, x = id & 7;
+    uint32_t t = x * (g.all >> 3) + (x < (g.all & 7) ? x : g.all & 7) + (id >> 3);
+    slice = g.part ? t / tiles : 0;
+    t -= slice * tiles;
     const uint32_t band = 8 * g.tiles_n, b = t / band, at = t - b * band;
     const uint32_t high = g.tiles_m - b * 8 < 8 ? g.tiles_m - b * 8 : 8;
     tn = at / high;
@@ -370,13 +378,11 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(Products p)
     const bool other = blockIdx.x >= p.second;
     const GemmArgs g = other ? p.g[1] : p.g[0];
     const Epilogue e = other ? p.e[1] : p.e[0];
-    const uint32_t ids = (g.tiles_m * g.tiles_n + 7) & ~7u;
-    uint32_t id = blockIdx.x + g.tile0 - (other ? p.second : 0), tm, tn;
-    const uint32_t slice = g.part ? id / ids : 0;
-    id -= slice * ids;
-    if (id >= g.tiles_m * g.tiles_n)
+    const uint32_t id = blockIdx.x + g.tile0 - (other ? p.second : 0);
+    uint32_t slice, tm, tn;
+    if (id >= g.all)
         return;
-    tile_place(g, id, tm, tn);
+    tile_place(g, id, slice, tm, tn);
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int64_t k0 = (int64_t)slice * g.steps * per_stage;
     const int64_t mine = (int64_t)g.steps * per_stage, depth = g.depth - k0 < mine ? g.depth - k0 : mine;
@@ -639,7 +645,9 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_gemm(Products p)
         epilogue(No());
 }
 
-// The slices' sums, added in order and finished: 4 columns a thread.  From
+// The slices' sums, added in order and finished: 4 columns a thread, BATCH of a
+// column's sums on their way at a time (bound by that chain: few threads, many
+// slices; 45 slices of 256 x 128: 7.5 us).  From
 // workgroup `second` on another product's.
 struct Join {
     const float* part[2];
@@ -649,7 +657,7 @@ struct Join {
     uint32_t second;
 };
 
-template <typename T>
+template <typename T, int BATCH>
 __global__ __launch_bounds__(256) void k_gemm_join(Join p)
 {
     const bool other = blockIdx.x >= p.second;
@@ -664,13 +672,13 @@ __global__ __launch_bounds__(256) void k_gemm_join(Join p)
         const int64_t m = all <= 0xffffffff ? (uint32_t)i / (uint32_t)per_row : i / per_row, n = (i - m * per_row) * 4;
         const int some = cols - n < 4 ? (int)(cols - n) : 4;
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s0 = 0; s0 < slices; s0 += 4) {
-            float x[4][4];
+        for (int s0 = 0; s0 < slices; s0 += BATCH) {
+            float x[BATCH][4];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < BATCH; ++u)
                 read_some<float, 4>(part + (s0 + u < slices ? s0 + u : s0) * size + m * cols + n, some, x[u]);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < BATCH; ++u)
                 if (s0 + u < slices) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
@@ -765,6 +773,11 @@ __global__ __launch_bounds__(512) void k_dbias(Products p)
 // is computed on the way, rounded to its type, and its unrounded column sums
 // per 64 rows kept for dbias.  Rows of the results are whole 16-byte pieces,
 // zeros behind their end.
+//
+// Bound by memory: 4096 x 2048 with gelu, X 4096 x 2048 and W 2048 x 2048 in
+// bfloat16, 117 MB read and written: 22 us, 5.3 TB/s.  (Reading the matrix
+// instructions' operands out of LDS the other way round would save the exchanged
+// copies, about half of that.)
 struct Turn {
     const void* src; // rows x cols
     int64_t ld, rows, cols;
@@ -883,8 +896,8 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
 // A tile of 256 x 256 moves half the bytes per product of one of 128 x 128 and
 // runs at 1.25 times its rate where there are enough of them (4096^3 bfloat16:
 // 116 us against 141), but only one fits a CU, so the last round of a product
-// with few tiles leaves more of the chip idle: 128 x 2048^2 x 2 and smaller
-// (4096 x 2048 x 2048: 55 us against 40) take the small one.
+// with few tiles leaves more of the chip idle: 4096 x 2048 x 2048 (128 large
+// tiles for 256 CUs: 55 us against 40) takes the small one.
 //
 // Small tiles run two to a CU with two stages each, which hides one's barriers
 // and epilogue behind the other's products; where there is at most one per CU it
@@ -916,36 +929,52 @@ int tile_for(const int64_t* rows, const int64_t* cols, const int64_t* stages, in
 int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return up(rows, tile) * up(cols, tile == 256 ? 256 : 128); }
 
 // How `n` products of one launch are cut: one tile for all, and slices of one
-// length, so that there is a workgroup for every CU.  A stage takes 0.34 us (1.35
-// in binary32, whose products take four times as long), writing, reading and
-// joining the sums some 4: slices are of at least 8 stages (2; 512 x 512 x 2048
-// binary16: 12.1 us against 13.7 with 4), and there are several only where that
-// shortens a workgroup by more than the join takes (64 x 4096 x 1024 bfloat16: 8.8
-// us as one, 10.9 as two; 128 x 512 x 4096: 21.6 as one, 11.3 as eight; 333 x 500 x
-// 1001 binary32: 43 and 16).
+// length, the length by an estimate of the time.  A stage of a tile takes a CU 0.34
+// us, or 0.58 with 128 rows (four times that in binary32): a launch with a
+// workgroup per CU at most takes as long as one slice, a larger one as long as the
+// work spread evenly and half a slice for the uneven end.  Slices cost the launch
+// that joins them, 4 us, and their sums' way to memory and back.
+//
+// 64 x 4096 x 1024 bfloat16: 8.8 us as one, 10.9 as two; 128 x 512 x 4096: 21.6 as
+// one, 11.3 as eight; 333 x 500 x 1001 binary32: 43 and 16; the gradient for M, N, K
+// = 16384, 512, 512 bfloat16, whose dW is 16 tiles of 256 stages beside 512 of 8: 172
+// whole, 57 sliced; 20000, 256, 128 binary32: 114 and 63.
 void shapes_of(const int64_t* rows, const int64_t* cols, const int64_t* depth, int n, int dtype, Shape* s)
 {
-    int64_t stages[2], most = 1, tiles = 0;
+    const int64_t least = dtype == kF32 ? 2 : 8; // stages
+    int64_t stages[2], most = 1;
+    double work = 0.0;
     for (int i = 0; i < n; ++i) {
         stages[i] = std::max<int64_t>(up(depth[i] * (int64_t)elem_bytes(dtype), kRow), 1);
         most = std::max(most, stages[i]);
     }
     const int tile = tile_for(rows, cols, stages, n, dtype);
     for (int i = 0; i < n; ++i)
-        tiles += tiles_of(rows[i], cols[i], tile);
+        work += (double)tiles_of(rows[i], cols[i], tile) * (double)stages[i];
     int64_t steps = most;
-    if (tile != 256 && tiles < kCus)
-        for (int64_t slices = 2; slices <= kCus; ++slices) {
+    if (tile != 256) {
+        const double stage_us = (tile == 64 ? 0.34 : 0.58) * (dtype == kF32 ? 4.0 : 1.0);
+        double best = 0.0;
+        // 1, 2, 3, 4, 6, 8, 12, ... slices of the deepest product
+        for (int64_t slices = 1, more = 1; slices <= kCus; slices += more, more = slices & (slices - 1) ? more : slices / 2) {
             const int64_t len = up(most, slices);
-            int64_t wgs = 0;
-            for (int i = 0; i < n; ++i)
-                wgs += tiles_of(rows[i], cols[i], tile) * up(stages[i], len);
-            if (wgs > kCus || len < (dtype == kF32 ? 2 : 8))
+            if (slices > 1 && len < least)
                 break;
-            steps = len;
+            double wgs = 0.0, sums = 0.0;
+            for (int i = 0; i < n; ++i) {
+                const double here = (double)up(stages[i], len);
+                wgs += (double)tiles_of(rows[i], cols[i], tile) * here;
+                sums += here > 1.0 ? here * (double)rows[i] * (double)cols[i] : 0.0;
+            }
+            const double span = wgs <= kCus ? (double)len
+                                            : std::max((double)len, work / (double)kCus + 0.5 * (double)len);
+            const double us = span * stage_us + (sums > 0.0 ? 4.0 + sums * 8.0 / 4e6 : 0.0);
+            if (slices == 1 || us < best) {
+                best = us;
+                steps = len;
+            }
         }
-    if (most - steps < (dtype == kF32 ? 3 : 12))
-        steps = most;
+    }
     int64_t groups = 0;
     for (int i = 0; i < n; ++i) {
         s[i].tile = tile;
@@ -992,7 +1021,8 @@ hipError_t gemm_launch(Products p, const Shape* s, int n, uint32_t sums, hipStre
     for (int i = 0; i < n; ++i) {
         p.g[i].tiles_m = (uint32_t)up(p.g[i].rows, BM);
         p.g[i].tiles_n = (uint32_t)up(p.g[i].cols, BN);
-        ids[i] = (uint32_t)up(p.g[i].tiles_m * p.g[i].tiles_n, 8) * 8 * (uint32_t)s[i].slices;
+        p.g[i].all = p.g[i].tiles_m * p.g[i].tiles_n * (uint32_t)s[i].slices;
+        ids[i] = (uint32_t)up(p.g[i].all, 8) * 8;
     }
     p.second = n > 1 ? ids[0] : kNoWork;
     p.sums = sums ? ids[0] + ids[1] : kNoWork;
@@ -1040,7 +1070,8 @@ hipError_t join(const Products& p, const Shape* s, int n, hipStream_t st)
     if (!m)
         return hipSuccess;
     j.second = m > 1 ? wgs[0] : kNoWork;
-    hipLaunchKernelGGL((k_gemm_join<T>), dim3(wgs[0] + wgs[1]), dim3(256), 0, st, j);
+    const bool many = std::max(j.slices[0], j.slices[1]) > 4; // slices in flight at a time
+    hipLaunchKernelGGL((many ? k_gemm_join<T, 16> : k_gemm_join<T, 4>), dim3(wgs[0] + wgs[1]), dim3(256), 0, st, j);
     return hipGetLastError();
 }
 
@@ -1080,7 +1111,7 @@ hipError_t gemm(GemmArgs g, const Epilogue& e, int dtype, void* part, hipStream_
 template <typename T>
 hipError_t linear_typed(const LinearLaunch& a, hipStream_t st)
 {
-    GemmArgs g{a.x, a.w, a.ldx, a.ldw, a.M, a.N, a.K, 0, 0, 0, 0, nullptr};
+    GemmArgs g{a.x, a.w, a.ldx, a.ldw, a.M, a.N, a.K, 0, 0, 0, 0, 0, nullptr};
     const Epilogue e{a.bias, a.residual, a.y, a.z, a.ldr, a.ldy, a.ldz, a.M, a.N, a.act,
                      near(std::max(a.ldr, std::max(a.ldy, a.ldz)), a.dtype)};
     return gemm<T>(g, e, a.dtype, a.work, st);
@@ -1158,10 +1189,10 @@ hipError_t grad_typed(const LinearGradLaunch& a, hipStream_t st)
         return err;
     // (where dZ lies in the workspace the zeros behind a row are part of it: whole pieces)
     Products p{};
-    p.g[0] = GemmArgs{as_is ? a.dy : w.dz, w.w_t, as_is ? a.lddy : w.Np, w.Np, a.M, a.K, as_is ? a.N : w.Np, 0, 0, 0, 0,
+    p.g[0] = GemmArgs{as_is ? a.dy : w.dz, w.w_t, as_is ? a.lddy : w.Np, w.Np, a.M, a.K, as_is ? a.N : w.Np, 0, 0, 0, 0, 0,
                       nullptr};
     p.e[0] = Epilogue{nullptr, nullptr, a.dx, nullptr, 0, a.lddx, 0, a.M, a.K, kNone, near(a.lddx, a.dtype)};
-    p.g[1] = GemmArgs{w.dz_t, w.x_t, w.Mp, w.Mp, a.N, a.K, w.Mp, 0, 0, 0, 0, nullptr};
+    p.g[1] = GemmArgs{w.dz_t, w.x_t, w.Mp, w.Mp, a.N, a.K, w.Mp, 0, 0, 0, 0, 0, nullptr};
     p.e[1] = Epilogue{nullptr, nullptr, a.dw, nullptr, 0, a.lddw, 0, a.N, a.K, kNone, near(a.lddw, a.dtype)};
     p.col_sums = (const float*)w.sums;
     p.row_tiles = up(a.M, 64);
@@ -1173,7 +1204,13 @@ hipError_t grad_typed(const LinearGradLaunch& a, hipStream_t st)
     if (both)
         grad_shapes(a.M, a.N, a.K, a.dtype, s);
     if (both && s->groups + sums < kMostWgs / 2) {
-        // both products and the column sums in one launch: the one fills what the other leaves idle
+        // both products and the column sums in one launch: the one fills what the other leaves idle, the deeper one
+        // first (its tiles take longer; the shorter ones then even out the end)
+        if (s[0].slices == 1 && s[1].slices == 1 && a.M > a.N) {
+            std::swap(p.g[0], p.g[1]);
+            std::swap(p.e[0], p.e[1]);
+            std::swap(s[0], s[1]);
+        }
         size_t at = 0;
         for (int i = 0; i < 2; ++i) {
             p.g[i].steps = s[i].steps;

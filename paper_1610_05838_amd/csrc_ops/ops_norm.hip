@@ -6,7 +6,10 @@
 // Bound by memory: a norm reads g once; clipping reads it again and writes it; a
 // step reads g again and p and writes p.  ONCE: gradients that are together
 // larger than the Infinity Cache are loaded past the caches, which have lost
-// their beginning by the time it is read again.
+// their beginning by the time it is read again (276 MB binary32: norm 45.7 us,
+// 6.0 TB/s, against 50.1; 1.6 GB: 230 against 258; 64 MB, which stay in the
+// caches: 15.2 against 14.5).  A step's update of 69 M binary32 parameters, 828 MB:
+// 128 us, 6.5 TB/s.
 //
 // Squares are summed in binary64 from the first: the square of a binary32 or
 // bfloat16 value leaves binary32's range at either end, a binary64 sum of such

@@ -134,7 +134,8 @@ def test_large_arguments():
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
-@pytest.mark.parametrize("m,n,k", [s for s in SHAPES if s != (4000, 3500, 520)] + [(4000, 1800, 520), (3000, 40, 3)])
+@pytest.mark.parametrize("m,n,k", [s for s in SHAPES if s != (4000, 3500, 520)] + [
+    (4000, 1800, 520), (3000, 40, 3), (20000, 40, 24), (9000, 260, 700), (40, 9000, 130)])
 @pytest.mark.parametrize("act,odd", [("none", False), ("none", True), ("relu", False), ("relu", True)])
 def test_linear_grad_is_the_exact_sum(dtype, m, n, k, act, odd):
     g = torch.Generator("cuda").manual_seed(m + n * 3 + k * 5)
