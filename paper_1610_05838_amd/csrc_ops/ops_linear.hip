@@ -1047,7 +1047,7 @@ hipError_t gemm_tiled(const Products& p, const Shape* s, int n, bool direct, uin
         return gemm_launch<T, 128, 128, 32, 64, false, 2>(p, s, n, sums, st);
     if (direct)
         return gemm_launch<T, 64, 128, 16, 64, true, 3>(p, s, n, sums, st);
-    return gemm_launch<T, 64, 128, 32, 64, false, 2>(p, s, n, sums, st);
+    return gemm_launch<T, 64, 128, 16, 64, false, 2>(p, s, n, sums, st);
 }
 
 // The slices of those products that have several, joined.
