@@ -143,3 +143,25 @@ def test_the_library_model_learns_from_a_batch():
     want = math.sqrt(float((r.double() - (P64[u.long()] * Q64[v.long()]).sum(1)).square().mean()))
     assert abs(M.rmse(samples) - want) <= 1e-5 * want
     M.finalize()
+
+
+def test_two_streams_at_once():
+    """Different operators enqueued in turn on two streams, nothing waited for between: what each gives alone."""
+    g = torch.Generator("cuda").manual_seed(6)
+    ids = torch.randint(-1, 500, (20_000,), generator=g, device="cuda", dtype=torch.int32)
+    rows = torch.randn(20_000, 72, generator=g, device="cuda")
+    x, w, dy = (torch.randn(a, b, generator=g, device="cuda") for a, b in ((3000, 200), (64, 200), (3000, 64)))
+    want_rows = M.embed_grad(rows, ids, 500)
+    want = M.linear_grad(dy, x, w)
+    want_norm = float(M.grad_norm([rows, x, w]))
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for n in range(12):
+        a, b = (one, two) if n % 2 else (two, one)
+        got.append((M.embed_grad(rows, ids, 500, stream=a), M.linear_grad(dy, x, w, stream=b),
+                    M.grad_norm([rows, x, w], stream=a)))
+    torch.cuda.synchronize()
+    for table, grads, norm in got:
+        assert torch.equal(table, want_rows) and float(norm) == want_norm
+        assert all(torch.equal(p, q) for p, q in zip(grads, want))
