@@ -6,6 +6,7 @@
 // Every product is one form, C = A B^T with A (rows x depth) and B (cols x
 // depth) both contiguous along the depth that is summed over.
 #include <algorithm>
+#include <cmath>
 
 #include "ops_common.hpp"
 
@@ -930,10 +931,10 @@ int64_t tiles_of(int64_t rows, int64_t cols, int tile) { return up(rows, tile) *
 
 // How `n` products of one launch are cut: one tile for all, and slices of one
 // length, the length by an estimate of the time.  A stage of a tile takes a CU 0.34
-// us, or 0.58 with 128 rows (four times that in binary32): a launch with a
-// workgroup per CU at most takes as long as one slice, a larger one as long as the
-// work spread evenly and half a slice for the uneven end.  Slices cost the launch
-// that joins them, 4 us, and their sums' way to memory and back.
+// us, or 0.58 with 128 rows (four times that in binary32): a product takes as many
+// slices as the fullest CU has, two unequal ones as long as the work spread evenly
+// and half a slice for the uneven end.  Slices cost the launch that joins them, 4
+// us, and their sums' way to memory and back, which has to stay in the caches.
 //
 // 64 x 4096 x 1024 bfloat16: 8.8 us as one, 10.9 as two; 128 x 512 x 4096: 21.6 as
 // one, 11.3 as eight; 333 x 500 x 1001 binary32: 43 and 16; the gradient for M, N, K
@@ -966,8 +967,12 @@ void shapes_of(const int64_t* rows, const int64_t* cols, const int64_t* depth, i
                 wgs += (double)tiles_of(rows[i], cols[i], tile) * here;
                 sums += here > 1.0 ? here * (double)rows[i] * (double)cols[i] : 0.0;
             }
-            const double span = wgs <= kCus ? (double)len
-                                            : std::max((double)len, work / (double)kCus + 0.5 * (double)len);
+            if (slices > 1 && sums * 4.0 > (double)kInfinityCache)
+                break;
+            const double rounds = std::ceil(wgs / (double)kCus);
+            const double span = n == 1 || rounds <= 1.0
+                                    ? rounds * (double)len
+                                    : std::max((double)len, work / (double)kCus + 0.5 * (double)len);
             const double us = span * stage_us + (sums > 0.0 ? 4.0 + sums * 8.0 / 4e6 : 0.0);
             if (slices == 1 || us < best) {
                 best = us;

@@ -186,6 +186,14 @@ def test_product_workspaces(lib):
         refused(lib, fn, (1, 1, 1, 0, None))
 
 
+def test_the_sums_of_slices_stay_within_the_caches(lib):
+    n = C.c_int64(-1)
+    for dtype in (0, 1, 2):
+        for sizes in ((4096, 4096, 1 << 20), (17, 17, INT32_MAX), (300, 5000, 1 << 24), (20_000, 20_000, 1 << 16)):
+            assert lib.mfsgd_linear_workspace(*sizes, dtype, C.byref(n)) == 0
+            assert 0 <= n.value <= 256 << 20
+
+
 def test_scores_need_a_model(lib):
     n = C.c_int64(-1)
     refused(lib, "mfsgd_scores_workspace", (5, C.byref(n)), ESTATE)
