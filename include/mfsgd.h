@@ -495,7 +495,8 @@ int mfsgd_debug_read(int32_t what, void* dst, int64_t count, void* stream);
  * them may run at once on different streams with workspaces of their own.
  *   - `dtype` is MFSGD_FP32, MFSGD_FP16 or MFSGD_BF16 (the operators alone:
  *     bfloat16); all arrays of a call have it.  Arithmetic and sums are
- *     binary32, each result is rounded once, to nearest even.
+ *     binary32, each result is rounded once, to nearest even (mfsgd_linear_grad
+ *     also rounds dZ on the way to dX and dW).
  *   - Matrices are row-major; `ld...` is the distance between rows in elements,
  *     at least the row's width.  A pointer needs the alignment of one element.
  *     Arrays must not overlap unless a call says they may.
@@ -570,7 +571,8 @@ int mfsgd_linear_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, int64
  * (the residual's gradient is dY).  dx, dw and dbias may be NULL: left out; z may
  * be NULL for MFSGD_ACT_NONE; w may be NULL without dx, x without dw.  The slope
  * of relu at 0 is 0, of an act at NaN is NaN.  dZ is rounded to the dtype before the products (as the
- * matrix instructions take it) and summed unrounded into dbias. */
+ * matrix instructions take it) and summed unrounded into dbias: with a 16-bit dtype and a sigmoid, silu or
+ * gelu, dX and dW then carry two roundings in place of one. */
 int mfsgd_linear_grad(const void* dy, int64_t lddy, const void* z, int64_t ldz, const void* x, int64_t ldx,
                       const void* w, int64_t ldw, int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t act,
                       void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias, void* workspace,
