@@ -577,6 +577,8 @@ int mfsgd_linear_grad(const void* dy, int64_t lddy, const void* z, int64_t ldz, 
                       const void* w, int64_t ldw, int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t act,
                       void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias, void* workspace,
                       int64_t workspace_bytes, void* stream);
+/* EINVAL also for sizes whose matrices are together larger than 2^62 bytes (here and in the call, whichever
+ * results it is asked for). */
 int mfsgd_linear_grad_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, int64_t* bytes);
 
 /* The model's answer: the scores of `count` users against all its items,

@@ -58,8 +58,16 @@ bool dtype_ok(int32_t d) { return d == kF32 || d == kF16 || d == kBF16; }
 
 constexpr int32_t kMostColumns = 1 << 22; // 64 to 512 columns a workgroup, on the grid's second axis
 
+int check_bytes(size_t need)
+{
+    REQUIRE(need <= kMostBytes, "the sizes ask for a workspace of more than 2^62 bytes");
+    return MFSGD_OK;
+}
+
 int check_work(const void* work, int64_t have, size_t need)
 {
+    if (int rc = check_bytes(need))
+        return rc;
     REQUIRE(need == 0 || (work && have >= 0 && (uint64_t)have >= need), "the workspace is too small");
     REQUIRE(need == 0 || aligned(work, 256), "the workspace is not aligned to 256 bytes");
     return MFSGD_OK;
@@ -381,7 +389,10 @@ int mfsgd_linear_grad_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, 
         REQUIRE(bytes, "NULL bytes");
         if (int rc = check_product(M, N, K, dtype))
             return rc;
-        *bytes = (int64_t)linear_grad_bytes(M, N, K, dtype);
+        const size_t need = linear_grad_bytes(M, N, K, dtype);
+        if (int rc = check_bytes(need))
+            return rc;
+        *bytes = (int64_t)need;
         return MFSGD_OK;
     });
 }

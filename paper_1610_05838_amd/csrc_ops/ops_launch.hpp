@@ -17,6 +17,20 @@ inline size_t elem_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
 // Workspaces are cut into parts that start at multiples of 256 bytes.
 inline size_t round256(size_t b) { return (b + 255) / 256 * 256; }
 
+// Sizes that no memory holds: sums and products of sizes stop at the largest
+// value, and a call whose workspace is above kMostBytes is refused.
+constexpr size_t kMostBytes = size_t(1) << 62;
+inline size_t times(size_t a, size_t b)
+{
+    size_t r;
+    return __builtin_mul_overflow(a, b, &r) ? SIZE_MAX : r;
+}
+inline size_t plus(size_t a, size_t b)
+{
+    size_t r;
+    return __builtin_add_overflow(a, b, &r) ? SIZE_MAX : r;
+}
+
 // ---- rows of a table (ops_rows.hip) ----
 struct RowsLaunch {
     const void* table;

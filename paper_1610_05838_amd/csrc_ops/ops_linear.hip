@@ -1148,19 +1148,19 @@ GradWork grad_work(int64_t M, int64_t N, int64_t K, int dtype, void* base)
     GradWork w;
     size_t at = 0;
     const size_t es = elem_bytes(dtype);
-    auto take = [&](size_t bytes) {
+    auto take = [&](size_t bytes) { // (an address is of use only where the sum is: the caller refuses others)
         char* p = (char*)base + at;
-        at += round256(bytes);
+        at = bytes > kMostBytes ? SIZE_MAX : plus(at, round256(bytes));
         return (void*)p;
     };
     const int64_t piece = 16 / (int64_t)es;
     w.Mp = up(M, piece) * piece;
     w.Np = up(N, piece) * piece;
-    w.dz = take(es * (size_t)M * (size_t)w.Np);
-    w.dz_t = take(es * (size_t)N * (size_t)w.Mp);
-    w.x_t = take(es * (size_t)K * (size_t)w.Mp);
-    w.w_t = take(es * (size_t)K * (size_t)w.Np);
-    w.sums = take(sizeof(float) * (size_t)up(M, 64) * (size_t)N);
+    w.dz = take(times(es * (size_t)M, (size_t)w.Np));
+    w.dz_t = take(times(es * (size_t)N, (size_t)w.Mp));
+    w.x_t = take(times(es * (size_t)K, (size_t)w.Mp));
+    w.w_t = take(times(es * (size_t)K, (size_t)w.Np));
+    w.sums = take(times(sizeof(float) * (size_t)up(M, 64), (size_t)N));
     size_t part = std::max(part_bytes(M, K, N, dtype), part_bytes(N, K, M, dtype));
     if (together(M, N, K)) {
         Shape s[2];
