@@ -1123,8 +1123,9 @@ template <typename T>
 hipError_t linear_typed(const LinearLaunch& a, hipStream_t st)
 {
     GemmArgs g{a.x, a.w, a.ldx, a.ldw, a.M, a.N, a.K, 0, 0, 0, 0, 0, nullptr};
+    // the pitch of a matrix that is left out was not checked and counts for nothing
     const Epilogue e{a.bias, a.residual, a.y, a.z, a.ldr, a.ldy, a.ldz, a.M, a.N, a.act,
-                     near(std::max(a.ldr, std::max(a.ldy, a.ldz)), a.dtype)};
+                     near(a.ldy, a.dtype) && (!a.residual || near(a.ldr, a.dtype)) && (!a.z || near(a.ldz, a.dtype))};
     return gemm<T>(g, e, a.dtype, a.work, st);
 }
 
