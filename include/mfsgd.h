@@ -499,15 +499,17 @@ int mfsgd_debug_read(int32_t what, void* dst, int64_t count, void* stream);
  *     also rounds dZ on the way to dX and dW).
  *   - Matrices are row-major; `ld...` is the distance between rows in elements,
  *     at least the row's width.  A pointer needs the alignment of one element.
- *     Arrays must not overlap unless a call says they may.
+ *     An array that is written must share no byte with another array of the
+ *     call (columns of one buffer may lie beside each other), unless the call
+ *     says that it may.
  *   - A workspace is device memory of at least the bytes that the matching
  *     ..._workspace call gives (0: none needed, NULL is fine), aligned to 256
  *     bytes; its content before and after is of no meaning.  It must not be
  *     used by anything else until the work enqueued on it has completed.
  *   - MFSGD_EINVAL for a negative size, a NULL array that has elements, an ld
- *     below the width, an unknown dtype, a pointer not aligned to its element
- *     and a workspace that is too small or misaligned; MFSGD_EHIP for a launch
- *     failure.  Nothing is enqueued on MFSGD_EINVAL. */
+ *     below the width, an unknown dtype, a pointer not aligned to its element,
+ *     arrays that overlap and a workspace that is too small or misaligned;
+ *     MFSGD_EHIP for a launch failure.  Nothing is enqueued on MFSGD_EINVAL. */
 enum { MFSGD_BF16 = 2 };
 
 /* Rows by id: out[i, 0..k) = scale * table[ids[i], 0..k) for i in [0, count).
@@ -612,16 +614,14 @@ typedef struct {
 /* The norm alone.  A tensor may appear more than once (it then counts so). */
 int mfsgd_grad_norm(const mfsgd_tensor* grads, int64_t count, double* norm_dev, void* workspace,
                     int64_t workspace_bytes, void* stream);
-/* g <- c g in place.  EINVAL also for a max_norm that is negative or NaN and for
- * tensors that overlap. */
+/* g <- c g in place.  EINVAL also for a max_norm that is negative or NaN. */
 int mfsgd_clip_grads(const mfsgd_tensor* grads, int64_t count, double max_norm, double* norm_dev, void* workspace,
                      int64_t workspace_bytes, void* stream);
 /* The clipped SGD update with the regularisation of section 2.2, in one pass:
  *   p <- p - lr * (c g + lambda p)
  * for params[i] and grads[i] of one n and dtype each; the gradients stay as they
  * are.  max_norm may be infinite (no clipping).  EINVAL also for a non-finite lr
- * or lambda, for params that overlap each other or any of grads, and for pairs
- * that differ in n or dtype. */
+ * or lambda and for pairs that differ in n or dtype. */
 int mfsgd_sgd_step(const mfsgd_tensor* params, const mfsgd_tensor* grads, int64_t count, float lr, float lambda,
                    double max_norm, double* norm_dev, void* workspace, int64_t workspace_bytes, void* stream);
 /* Workspace of the three for up to `count` tensors. */

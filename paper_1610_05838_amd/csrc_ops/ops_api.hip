@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -73,6 +74,82 @@ int check_work(const void* work, int64_t have, size_t need)
     return MFSGD_OK;
 }
 
+// What a call reads or writes: rows of `width` bytes, `pitch` bytes apart.
+struct Area {
+    uintptr_t at;
+    int64_t rows, width, pitch;
+    bool written;
+
+    uintptr_t end() const { return at + (uintptr_t)((rows - 1) * pitch + width); }
+};
+
+Area matrix(const void* p, int64_t rows, int64_t width, int64_t ld, int dtype, bool written = false)
+{
+    const int64_t es = (int64_t)elem_bytes(dtype);
+    if (!p || rows == 0 || width == 0)
+        return Area{0, 0, 0, 0, false};
+    if (rows == 1 || ld == width)
+        return Area{(uintptr_t)p, 1, rows * width * es, rows * width * es, written};
+    return Area{(uintptr_t)p, rows, width * es, ld * es, written};
+}
+
+Area row(const void* p, int64_t n, int dtype, bool written = false) { return matrix(p, 1, n, n, dtype, written); }
+
+Area ids_area(const int32_t* ids, int64_t stride, int64_t count) { return matrix(ids, count, 1, stride, kF32); }
+
+Area bytes_area(const void* p, size_t bytes) // a workspace
+{
+    return Area{(uintptr_t)p, p && bytes ? 1 : 0, (int64_t)bytes, (int64_t)bytes, true};
+}
+
+// Whether [from, to) holds a byte of a.
+bool reaches(const Area& a, uintptr_t from, uintptr_t to)
+{
+    if (to <= a.at || from >= a.end())
+        return false;
+    // the first row that ends behind `from`
+    const int64_t i = from < a.at + (uintptr_t)a.width ? 0 : (int64_t)(from - a.at - (uintptr_t)a.width) / a.pitch + 1;
+    return i < a.rows && a.at + (uintptr_t)(i * a.pitch) < to;
+}
+
+// Whether the two share a byte.  Columns of one buffer lie inside each other's
+// extent without doing so: with equal pitches the remainders of their starts
+// tell; otherwise the rows of one are looked for in the other, which ends at the
+// first that is there.
+bool share(const Area& a, const Area& b)
+{
+    if (a.rows == 0 || b.rows == 0 || a.end() <= b.at || b.end() <= a.at)
+        return false;
+    if (a.rows == 1)
+        return reaches(b, a.at, a.end());
+    if (b.rows == 1)
+        return reaches(a, b.at, b.end());
+    if (a.pitch == b.pitch) {
+        const uintptr_t pitch = (uintptr_t)a.pitch;
+        const uintptr_t behind = b.at >= a.at ? (b.at - a.at) % pitch : (pitch - (a.at - b.at) % pitch) % pitch;
+        if (behind >= (uintptr_t)a.width && behind + (uintptr_t)b.width <= pitch)
+            return false;
+    }
+    const Area &few = a.rows < b.rows ? a : b, &other = a.rows < b.rows ? b : a;
+    const int64_t skip = few.at < other.at ? (int64_t)(other.at - few.at) / few.pitch : 0;
+    for (int64_t i = skip; i < few.rows; ++i) {
+        const uintptr_t at = few.at + (uintptr_t)(i * few.pitch);
+        if (at >= other.end())
+            break;
+        if (reaches(other, at, at + (uintptr_t)few.width))
+            return true;
+    }
+    return false;
+}
+
+int check_apart(std::initializer_list<Area> all)
+{
+    for (const Area* a = all.begin(); a != all.end(); ++a)
+        for (const Area* b = a + 1; b != all.end(); ++b)
+            REQUIRE(!(a->written || b->written) || !share(*a, *b), "an array that is written overlaps another one");
+    return MFSGD_OK;
+}
+
 int check_ids(const int32_t* ids, int64_t stride, int64_t count)
 {
     REQUIRE(count >= 0 && count <= INT32_MAX, "count must be in [0, 2^31-1]");
@@ -90,6 +167,9 @@ int embed_impl(const RowsLaunch& a, void* stream)
         return rc;
     REQUIRE(matrix_ok(a.table, a.rows, a.k, a.ld, a.dtype), "table is NULL or misaligned, or ld is below k");
     REQUIRE(matrix_ok(a.out, a.count, a.k, a.ld_out, a.dtype), "out is NULL or misaligned, or ld_out is below k");
+    if (int rc = check_apart({matrix(a.table, a.rows, a.k, a.ld, a.dtype), ids_area(a.ids, a.ids_stride, a.count),
+                              matrix(a.out, a.count, a.k, a.ld_out, a.dtype, true)}))
+        return rc;
     return a.count ? launched(rows_get(a, (hipStream_t)stream)) : MFSGD_OK;
 }
 
@@ -102,7 +182,12 @@ int embed_grad_impl(RowsGradLaunch a, void* work, int64_t bytes, void* stream)
         return rc;
     REQUIRE(matrix_ok(a.dout, a.count, a.k, a.ld_dout, a.dtype), "dout is NULL or misaligned, or ld_dout is below k");
     REQUIRE(matrix_ok(a.dtable, a.rows, a.k, a.ld, a.dtype), "dtable is NULL or misaligned, or ld is below k");
-    if (int rc = check_work(work, bytes, rows_grad_bytes(a.count, a.k)))
+    const size_t need = rows_grad_bytes(a.count, a.k);
+    if (int rc = check_work(work, bytes, need))
+        return rc;
+    if (int rc = check_apart({matrix(a.dout, a.count, a.k, a.ld_dout, a.dtype),
+                              ids_area(a.ids, a.ids_stride, a.count),
+                              matrix(a.dtable, a.rows, a.k, a.ld, a.dtype, true), bytes_area(work, need)}))
         return rc;
     a.work = work;
     return launched(rows_grad(a, (hipStream_t)stream));
@@ -145,7 +230,15 @@ int linear_impl(LinearLaunch a, void* work, int64_t bytes, void* stream)
             "residual is misaligned, or ldr is below N");
     REQUIRE(matrix_ok(a.y, a.M, a.N, a.ldy, a.dtype), "y is NULL or misaligned, or ldy is below N");
     REQUIRE(!a.z || matrix_ok(a.z, a.M, a.N, a.ldz, a.dtype), "z is misaligned, or ldz is below N");
-    if (int rc = check_work(work, bytes, linear_bytes(a.M, a.N, a.K, a.dtype)))
+    const size_t need = linear_bytes(a.M, a.N, a.K, a.dtype);
+    if (int rc = check_work(work, bytes, need))
+        return rc;
+    const bool in_place = a.residual == a.y && (a.ldr == a.ldy || a.M == 1);
+    if (int rc = check_apart({matrix(a.x, a.M, a.K, a.ldx, a.dtype), matrix(a.w, a.N, a.K, a.ldw, a.dtype),
+                              row(a.bias, a.N, a.dtype),
+                              matrix(in_place ? nullptr : a.residual, a.M, a.N, a.ldr, a.dtype),
+                              matrix(a.y, a.M, a.N, a.ldy, a.dtype, true), matrix(a.z, a.M, a.N, a.ldz, a.dtype, true),
+                              bytes_area(work, need)}))
         return rc;
     a.work = work;
     return launched(linear(a, (hipStream_t)stream));
@@ -164,7 +257,16 @@ int linear_grad_impl(LinearGradLaunch a, void* work, int64_t bytes, void* stream
     REQUIRE(!a.dx || matrix_ok(a.dx, a.M, a.K, a.lddx, a.dtype), "dx is misaligned, or lddx is below K");
     REQUIRE(!a.dw || matrix_ok(a.dw, a.N, a.K, a.lddw, a.dtype), "dw is misaligned, or lddw is below K");
     REQUIRE(aligned(a.dbias, elem_bytes(a.dtype)), "dbias is misaligned");
-    if (int rc = check_work(work, bytes, linear_grad_bytes(a.M, a.N, a.K, a.dtype)))
+    const size_t need = linear_grad_bytes(a.M, a.N, a.K, a.dtype);
+    if (int rc = check_work(work, bytes, need))
+        return rc;
+    if (int rc = check_apart({matrix(a.dy, a.M, a.N, a.lddy, a.dtype),
+                              matrix(a.act == MFSGD_ACT_NONE ? nullptr : a.z, a.M, a.N, a.ldz, a.dtype),
+                              matrix(a.dw ? a.x : nullptr, a.M, a.K, a.ldx, a.dtype),
+                              matrix(a.dx ? a.w : nullptr, a.N, a.K, a.ldw, a.dtype),
+                              matrix(a.dx, a.M, a.K, a.lddx, a.dtype, true),
+                              matrix(a.dw, a.N, a.K, a.lddw, a.dtype, true), row(a.dbias, a.N, a.dtype, true),
+                              bytes_area(work, need)}))
         return rc;
     a.work = work;
     return launched(linear_grad(a, (hipStream_t)stream));
@@ -193,11 +295,15 @@ int scores_impl(const int32_t* users, int64_t stride, int64_t count, int64_t n, 
     REQUIRE(act >= MFSGD_ACT_NONE && act <= MFSGD_ACT_GELU, "unknown act");
     REQUIRE(aligned(bias, elem_bytes(dtype)), "bias is misaligned");
     REQUIRE(matrix_ok(out, count, n, ld_out, dtype), "out is NULL or misaligned, or ld_out is below n");
-    const size_t rows = scores_rows_bytes(v, count);
-    if (int rc = check_work(work, bytes, rows + linear_bytes(count, n, v.KP, dtype)))
+    const size_t rows = scores_rows_bytes(v, count), need = rows + linear_bytes(count, n, v.KP, dtype);
+    if (int rc = check_work(work, bytes, need))
         return rc;
     if (count == 0)
         return MFSGD_OK;
+    if (int rc = check_apart({ids_area(users, stride, count), row(bias, n, dtype), matrix(P, m, v.KP, v.KP, dtype),
+                              matrix(v.Q, n, v.KP, v.KP, dtype), matrix(out, count, n, ld_out, dtype, true),
+                              bytes_area(work, need)}))
+        return rc;
     if (int rc = embed_impl(RowsLaunch{P, m, v.KP, v.KP, dtype, users, stride, count, 1.0f, work, v.KP}, stream))
         return rc;
     return linear_impl(LinearLaunch{work, v.Q, bias, nullptr, v.KP, v.KP, 0, count, n, v.KP, dtype, act, out, nullptr,
@@ -269,16 +375,17 @@ int norm_impl(const mfsgd_tensor* params, const mfsgd_tensor* grads, int64_t cou
             REQUIRE(params[i].n == grads[i].n && params[i].dtype == grads[i].dtype,
                     "a parameter and its gradient differ in size or dtype");
     }
-    if (int rc = check_work(work, bytes, norm_bytes(count)))
+    const size_t need = norm_bytes(count);
+    if (int rc = check_work(work, bytes, need))
         return rc;
-    if (apply) {
-        std::vector<Span> spans;
-        spans.reserve((size_t)count * 2);
-        add_spans(spans, grads, count, apply == 1);
-        if (apply == 2)
-            add_spans(spans, params, count, true);
-        REQUIRE(!overlap(spans), "tensors that are written overlap others");
-    }
+    std::vector<Span> spans;
+    spans.reserve((size_t)count * 2 + 2);
+    add_spans(spans, grads, count, apply == 1);
+    if (apply == 2)
+        add_spans(spans, params, count, true);
+    spans.push_back(Span{(uintptr_t)norm_dev, (uintptr_t)norm_dev + sizeof(double), true});
+    spans.push_back(Span{(uintptr_t)work, (uintptr_t)work + need, true});
+    REQUIRE(!overlap(spans), "an array that is written overlaps another one");
     std::vector<NormTensor> list((size_t)count);
     for (int64_t i = 0; i < count; ++i)
         list[i] = NormTensor{apply == 2 ? params[i].data : grads[i].data, grads[i].data, grads[i].n, grads[i].dtype};

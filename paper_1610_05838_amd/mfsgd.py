@@ -301,9 +301,11 @@ def debug_priority(s: int, stream=None):
 #
 # Outputs and workspaces not passed in are allocated on the stream the work runs
 # on; tensors given to a call on another stream than the current one may be
-# freed right after it (the order of work on the two is the caller's).  Row-major matrices may have any row pitch; a tensor on another device
-# than the current one, of another dtype than its call's or with strided
-# columns is refused before anything is enqueued.
+# freed right after it (the order of work on the two is the caller's).  Row-major
+# matrices may have any row pitch; a tensor on another device than the current
+# one, of another dtype than its call's or with strided columns is refused
+# before anything is enqueued, and so is an `out` that shares memory with what
+# the call reads, unless it says that it may.
 
 _DTYPES = {torch.float32: FP32, torch.float16: FP16, torch.bfloat16: BF16}
 
