@@ -79,6 +79,10 @@ __device__ __forceinline__ void activate(float (&v)[C], int act)
     }
 }
 
+// Beyond 128 on either side a result or slope equals its limit in every type, and
+// the formulas' products of an infinity and a zero become that limit.  NaN stays.
+__device__ __forceinline__ float bounded(float z) { return z < -128.0f ? -128.0f : z > 128.0f ? 128.0f : z; }
+
 template <bool EXACT>
 __device__ __forceinline__ float slope(float z, int act)
 {
@@ -90,10 +94,12 @@ __device__ __forceinline__ float slope(float z, int act)
         return s * (1.0f - s);
     }
     case kSilu: {
+        z = bounded(z);
         const float s = sigmoid<EXACT>(z);
         return s * (1.0f + z * (1.0f - s));
     }
     case kGelu: {
+        z = bounded(z);
         const float e = EXACT ? expf(-0.5f * z * z) : __expf(-0.5f * z * z);
         return normal_cdf<EXACT>(z) + z * e * 0.39894228040143268f;
     }

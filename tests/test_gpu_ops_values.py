@@ -58,47 +58,3 @@ def test_a_layer_whose_pre_activation_leaves_binary16(act, m):
     assert bool((dx == 1000.0).all())
     assert bool((dw[::2] == 0.0).all()) and bool((dw[1::2] == 100.0 * m).all())
     assert bool((db[::2] == 0.0).all()) and bool((db[1::2] == m).all())
-
-
-@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
-@pytest.mark.parametrize("act", ["sigmoid", "silu", "gelu"])
-def test_a_column_masked_by_minus_infinity_is_zero(dtype, act):
-    """A bias of -inf, or of the lowest value of the type, takes a column out."""
-    for m, n, k in ((3, 50, 24), (200, 300, 72), (40, 30, 13)):
-        x, w = torch.ones(m, k, dtype=dtype, device="cuda"), torch.ones(n, k, dtype=dtype, device="cuda")
-        bias = torch.zeros(n, dtype=dtype, device="cuda")
-        bias[2::3], bias[1::3] = -INF, torch.finfo(dtype).min
-        y = M.linear(x, w, bias=bias, act=act)
-        assert bool((y[:, 2::3] == 0.0).all()) and bool((y[:, 1::3] == 0.0).all()) and bool((y[:, ::3] > 0.5).all())
-        bias[2::3] = math.nan
-        assert bool(torch.isnan(M.linear(x, w, bias=bias, act=act)[:, 2::3]).all())
-
-
-def tail_points(dtype, low, high):
-    z = torch.linspace(low, high, 3001, device="cuda").to(dtype)
-    return z, z.double()
-
-
-@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
-def test_gelu_lower_tail(dtype):
-    """Relative to its own size.  16 bits: the normal distribution's tail to 3e-5; all: z^2 2^-22 of exp(-z^2 / 2),
-    whose argument is rounded, and a few roundings."""
-    z, z64 = tail_points(dtype, -12.5, -1.5)
-    cdf = 0.5 * torch.erfc(-z64 / math.sqrt(2.0))
-    density = torch.exp(-0.5 * z64 * z64) / math.sqrt(2.0 * math.pi)
-    own = (z64 * z64 + 16.0) * 2.0**-22 + (0.0 if dtype == torch.float32 else 3e-5)
-    y, slope = through(z, "gelu")
-    assert within(y, z64 * cdf, dtype, own)
-    # the slope's two terms have different signs: each is off by `own` of itself
-    want = cdf + z64 * density
-    assert within(slope, want, dtype, own * ((cdf + z64.abs() * density) / want.abs()))
-
-
-@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
-def test_sigmoid_slope_in_both_tails(dtype):
-    """exp(-|z|) / (1 + exp(-|z|))^2, relative to its own size: the exponential to (|z| + 2) 2^-23, a few roundings."""
-    for low, high in ((-16.0, -1.0), (1.0, 16.0), (20.0, 80.0)):
-        z, z64 = tail_points(dtype, low, high)
-        e = torch.exp(-z64.abs())
-        _, slope = through(z, "sigmoid")
-        assert within(slope, e / (1.0 + e)**2, dtype, (z64.abs() + 16.0) * 2.0**-22)
