@@ -554,7 +554,8 @@ int mfsgd_add_rows(int32_t side, const void* dout, int64_t ld_dout, const int32_
  * X is M x K, W N x K (a row per output, as Q has a row per item), Y, Z and
  * residual M x N, bias N values (contiguous).  bias, residual and z may be NULL:
  * left out.  z receives the pre-activation for the gradient.  The epilogue works
- * on the binary32 sums; Z and Y are each rounded once.  residual may be y itself
+ * on the binary32 sums; Z and Y are each rounded once; at an infinite Z an act is
+ * its limit (a bias of -infinity takes a column out).  residual may be y itself
  * (same pointer and ld).  Any M, N, K in [0, 2^31-1] (K = 0: Z = bias). */
 enum {
     MFSGD_ACT_NONE = 0,    /* Z */

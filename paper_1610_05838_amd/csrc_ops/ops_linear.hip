@@ -52,6 +52,11 @@ __device__ __forceinline__ float normal_cdf(float z) // (1 + erf(z / sqrt 2)) / 
     return z < 0.0f ? tail : 1.0f - tail;
 }
 
+// Beyond 128 on either side a result or slope equals its limit in every type, and
+// the formulas' products of an infinity and a zero become that limit.  NaN stays.
+__device__ __forceinline__ float above(float z) { return z < -128.0f ? -128.0f : z; }
+__device__ __forceinline__ float bounded(float z) { return z < -128.0f ? -128.0f : z > 128.0f ? 128.0f : z; }
+
 template <bool EXACT, int C>
 __device__ __forceinline__ void activate(float (&v)[C], int act)
 {
@@ -69,19 +74,15 @@ __device__ __forceinline__ void activate(float (&v)[C], int act)
     case kSilu:
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            v[c] = v[c] * sigmoid<EXACT>(v[c]);
+            v[c] = above(v[c]) * sigmoid<EXACT>(v[c]);
         break;
     case kGelu:
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            v[c] = v[c] * normal_cdf<EXACT>(v[c]);
+            v[c] = above(v[c]) * normal_cdf<EXACT>(v[c]);
         break;
     }
 }
-
-// Beyond 128 on either side a result or slope equals its limit in every type, and
-// the formulas' products of an infinity and a zero become that limit.  NaN stays.
-__device__ __forceinline__ float bounded(float z) { return z < -128.0f ? -128.0f : z > 128.0f ? 128.0f : z; }
 
 template <bool EXACT>
 __device__ __forceinline__ float slope(float z, int act)

@@ -58,3 +58,17 @@ def test_a_layer_whose_pre_activation_leaves_binary16(act, m):
     assert bool((dx == 1000.0).all())
     assert bool((dw[::2] == 0.0).all()) and bool((dw[1::2] == 100.0 * m).all())
     assert bool((db[::2] == 0.0).all()) and bool((db[1::2] == m).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
+@pytest.mark.parametrize("act", ["sigmoid", "silu", "gelu"])
+def test_a_column_masked_by_minus_infinity_is_zero(dtype, act):
+    """A bias of -inf, or of the lowest value of the type, takes a column out."""
+    for m, n, k in ((3, 50, 24), (200, 300, 72), (40, 30, 13)):
+        x, w = torch.ones(m, k, dtype=dtype, device="cuda"), torch.ones(n, k, dtype=dtype, device="cuda")
+        bias = torch.zeros(n, dtype=dtype, device="cuda")
+        bias[2::3], bias[1::3] = -INF, torch.finfo(dtype).min
+        y = M.linear(x, w, bias=bias, act=act)
+        assert bool((y[:, 2::3] == 0.0).all()) and bool((y[:, 1::3] == 0.0).all()) and bool((y[:, ::3] > 0.5).all())
+        bias[2::3] = math.nan
+        assert bool(torch.isnan(M.linear(x, w, bias=bias, act=act)[:, 2::3]).all())
