@@ -72,3 +72,23 @@ def test_a_column_masked_by_minus_infinity_is_zero(dtype, act):
         assert bool((y[:, 2::3] == 0.0).all()) and bool((y[:, 1::3] == 0.0).all()) and bool((y[:, ::3] > 0.5).all())
         bias[2::3] = math.nan
         assert bool(torch.isnan(M.linear(x, w, bias=bias, act=act)[:, 2::3]).all())
+
+
+def tail_points(dtype, low, high):
+    z = torch.linspace(low, high, 3001, device="cuda").to(dtype)
+    return z, z.double()
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
+def test_gelu_lower_tail(dtype):
+    """Relative to its own size.  16 bits: the normal distribution's tail to 3e-5; all: z^2 2^-22 of exp(-z^2 / 2),
+    whose argument is rounded, and a few roundings."""
+    z, z64 = tail_points(dtype, -12.5, -1.5)
+    cdf = 0.5 * torch.erfc(-z64 / math.sqrt(2.0))
+    density = torch.exp(-0.5 * z64 * z64) / math.sqrt(2.0 * math.pi)
+    own = (z64 * z64 + 16.0) * 2.0**-22 + (0.0 if dtype == torch.float32 else 3e-5)
+    y, slope = through(z, "gelu")
+    assert within(y, z64 * cdf, dtype, own)
+    # the slope's two terms have different signs: each is off by `own` of itself
+    want = cdf + z64 * density
+    assert within(slope, want, dtype, own * ((cdf + z64.abs() * density) / want.abs()))
