@@ -58,10 +58,11 @@ __device__ __forceinline__ float normal_cdf(float z) // (1 + erf(z / sqrt 2)) / 
     return z < 0.0f ? tail : 1.0f - tail;
 }
 
-// Beyond 128 on either side a result or slope equals its limit in every type, and
-// the formulas' products of an infinity and a zero become that limit.  NaN stays.
-__device__ __forceinline__ float above(float z) { return z < -128.0f ? -128.0f : z; }
-__device__ __forceinline__ float bounded(float z) { return z < -128.0f ? -128.0f : z > 128.0f ? 128.0f : z; }
+// Beyond 128 on either side a result or slope equals its limit in every type; with
+// z bounded there the formulas' products of an infinity and a zero become that
+// limit.  (A NaN is lost in the bound and comes back with the other factor.)
+__device__ __forceinline__ float above(float z) { return fmaxf(z, -128.0f); }
+__device__ __forceinline__ float bounded(float z) { return __builtin_amdgcn_fmed3f(z, -128.0f, 128.0f); }
 
 template <bool EXACT, int C>
 __device__ __forceinline__ void activate(float (&v)[C], int act)
@@ -101,14 +102,12 @@ __device__ __forceinline__ float slope(float z, int act)
         return s * (1.0f - s);
     }
     case kSilu: {
-        z = bounded(z);
         const float s = sigmoid<EXACT>(z);
-        return s * (1.0f + z * (1.0f - s));
+        return s * (1.0f + bounded(z) * (1.0f - s));
     }
     case kGelu: {
-        z = bounded(z);
         const float e = EXACT ? expf(-0.5f * z * z) : __expf(-0.5f * z * z);
-        return normal_cdf<EXACT>(z) + z * e * 0.39894228040143268f;
+        return normal_cdf<EXACT>(z) + bounded(z) * e * 0.39894228040143268f;
     }
     default:
         return 1.0f;
