@@ -97,9 +97,10 @@ __device__ __forceinline__ float slope(float z, int act)
     switch (act) {
     case kRelu:
         return z > 0.0f ? 1.0f : z != z ? z : 0.0f; // a NaN stays one, as in the result
-    case kSigmoid: {
-        const float s = sigmoid<EXACT>(z);
-        return s * (1.0f - s);
+    case kSigmoid: { // s (1 - s) without the difference: the same on both sides of 0
+        const float e = EXACT ? expf(-fabsf(z)) : __expf(-fabsf(z));
+        const float r = EXACT ? 1.0f / (1.0f + e) : __builtin_amdgcn_rcpf(1.0f + e);
+        return e * r * r;
     }
     case kSilu: {
         const float s = sigmoid<EXACT>(z);

@@ -92,3 +92,13 @@ def test_gelu_lower_tail(dtype):
     # the slope's two terms have different signs: each is off by `own` of itself
     want = cdf + z64 * density
     assert within(slope, want, dtype, own * ((cdf + z64.abs() * density) / want.abs()))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
+def test_sigmoid_slope_in_both_tails(dtype):
+    """exp(-|z|) / (1 + exp(-|z|))^2, relative to its own size: the exponential to (|z| + 2) 2^-23, a few roundings."""
+    for low, high in ((-16.0, -1.0), (1.0, 16.0), (20.0, 80.0)):
+        z, z64 = tail_points(dtype, low, high)
+        e = torch.exp(-z64.abs())
+        _, slope = through(z, "sigmoid")
+        assert within(slope, e / (1.0 + e)**2, dtype, (z64.abs() + 16.0) * 2.0**-22)
