@@ -932,14 +932,20 @@ struct Shape {
 // The tile for `n` products of one launch.
 int tile_for(const int64_t* rows, const int64_t* cols, const int64_t* stages, int n, int dtype)
 {
-    int64_t big = 0, mid = 0, low = 0, least = stages[0];
+    int64_t big = 0, mid = 0, low = 0, least = stages[0], most = 0, work = 0;
     for (int i = 0; i < n; ++i) {
         big += up(rows[i], 256) * up(cols[i], 256);
+        work += up(rows[i], 256) * up(cols[i], 256) * stages[i];
+        most = std::max(most, stages[i]);
         mid += up(rows[i], 128) * up(cols[i], 128);
         low += up(rows[i], 64) * up(cols[i], 128);
         least = std::min(least, stages[i]);
     }
-    if (least >= 8 && (double)up(big, kCus) <= 0.625 * 0.5 * (double)up(mid, kCus))
+    // Large tiles have no slices, so of two products the deeper one's tiles must not be what the launch waits for: up to
+    // 1.25 times the evenly spread stages, which is the rate they gain.  (M, N, K = 24576, 512, 512 bfloat16, where dW is
+    // 4 such tiles of 384 stages: 443 us, 65 with tiles of 128 and slices; 6144, 2048, 2048: 146 and 117.)
+    const bool even = n == 1 || (double)most * (double)kCus <= 1.25 * (double)work;
+    if (least >= 8 && even && (double)up(big, kCus) <= 0.625 * 0.5 * (double)up(mid, kCus))
         return 256;
     // Tiles of 64 rows where they fill the last round better: one takes 0.55 of the other's time in binary32, 0.7 in
     // 16 bits (bound by what comes from L2), measured on 1000 x 5000 x 776 (88 us against 112; 21.6 against 20).

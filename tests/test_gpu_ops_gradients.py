@@ -1,0 +1,67 @@
+"""The product's gradient where its two products differ much in size or depth:
+dX has the batch as its rows, dW as its depth.
+
+Small integers again, whose sums are exact in any order.  Times are compared
+with those of the same work cut otherwise, with room for a factor."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+from paper_1610_05838_amd import mfsgd as M  # noqa: E402
+
+DTYPES = (torch.float32, torch.float16, torch.bfloat16)
+ID = {torch.float32: "fp32", torch.float16: "fp16", torch.bfloat16: "bf16"}
+
+
+def ints(g, low, high, *shape):
+    return torch.randint(low, high + 1, shape, generator=g, device="cuda")
+
+
+def exact(m, n, k, dtype, act="relu"):
+    g = torch.Generator("cuda").manual_seed(m + n + k)
+    x, w, dy, z = (ints(g, -2, 2, *s).to(dtype) for s in ((m, k), (n, k), (m, n), (m, n)))
+    dz = dy.double() * (z > 0)
+    dx, dw, db = M.linear_grad(dy, x, w, z=z, act=act)
+    assert torch.equal(dx, (dz @ w.double()).to(dtype))
+    assert torch.equal(dw, (dz.t().contiguous() @ x.double()).to(dtype))
+    assert torch.equal(db, dz.sum(0).to(dtype))
+    again = M.linear_grad(dy, x, w, z=z, act=act)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dw) and torch.equal(again[2], db)
+
+
+def microseconds(call):
+    for _ in range(3):
+        call()
+    best = float("inf")
+    for _ in range(5):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(5):
+            call()
+        b.record()
+        b.synchronize()
+        best = min(best, a.elapsed_time(b) * 200.0)
+    return best
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
+@pytest.mark.parametrize("m,n,k", [(2800, 2790, 2816), (3100, 2490, 2810), (24_576, 512, 512), (24_600, 500, 520),
+                                   (6144, 512, 2048)])
+def test_gradients_of_large_layers(dtype, m, n, k):
+    """The first two run in tiles of 256 rows, both products and the bias in one launch; the others have so long a
+    batch that dW's few tiles are cut along their depth."""
+    exact(m, n, k, dtype)
+
+
+@pytest.mark.parametrize("m,n,k", [(24_576, 512, 512), (16_384, 768, 768), (12_288, 1024, 1024)])
+def test_a_long_batch_costs_its_work(m, n, k):
+    """One gradient of a batch takes at most 1.5 times those of its halves together."""
+    g = torch.Generator("cuda").manual_seed(1)
+    x, w, dy = (torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((m, k), (n, k), (m, n)))
+    whole = microseconds(lambda: M.linear_grad(dy, x, w))
+    half = microseconds(lambda: M.linear_grad(dy[:m // 2], x[:m // 2], w))
+    assert whole <= 1.5 * 2 * half, (whole, half)
