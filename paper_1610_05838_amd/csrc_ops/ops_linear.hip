@@ -703,7 +703,7 @@ __global__ __launch_bounds__(256) void k_gemm_join(Join p)
     }
 }
 
-// Up to 16 rows (a batch of queries, a single token): bound by reading B, which
+// Up to 16 rows (a batch of queries, a single token; see few_rows): bound by reading B, which
 // goes from memory to the matrix instructions' registers without a stop in LDS
 // (one row against 4096 x 4096 bfloat16 in the caches: 8.2 us, 4.1 TB/s; with the
 // tiles above 10.3), and by the latency of a launch and one trip to memory where B
@@ -923,7 +923,7 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
 // and epilogue behind the other's products; where there is at most one per CU it
 // gets the LDS of both as four stages (2048 x 2048 x 4096: 37 us against 48).
 struct Shape {
-    int tile;       // 0: few rows; else rows of a tile
+    int tile;       // 0: k_gemm_few; else rows of a tile
     int slices;     // > 1: sums to the workspace, joined afterwards
     int steps;      // stages of a slice
     int64_t groups; // workgroups
@@ -1016,10 +1016,20 @@ void shapes_of(const int64_t* rows, const int64_t* cols, const int64_t* depth, i
         s[i].groups = groups;
 }
 
+// Up to 16 rows have a kernel of their own (k_gemm_few), which reads B once but
+// splits no depth over workgroups: 16 columns each, so that up to 2048 columns
+// leave half the chip idle while a wavefront goes down a quarter of the depth.  Of
+// such a product at least 8192 deep the tiles take slices.  16 rows, columns x
+// depth, bfloat16: 512 x 4096 4.6 us there, 8.7 in tiles (8192 deep: 16.6 and 9.5;
+// 32,768: 58 and 15); 2048 x 8192: 17.2 and 11.4; 4096 x 8192: 17.9 and 17.4.  One
+// row, binary32: 1024 x 4096 11.4 and 12.5; 2048 x 8192 28.9 and 25.2; 3000 x 8192
+// 29.8 and 36.5.  dW of one output over a batch of 10^6 is of this form.
+bool few_rows(int64_t rows, int64_t cols, int64_t depth) { return rows <= 16 && (depth < 8192 || cols > 2048); }
+
 Shape shape_of(int64_t rows, int64_t cols, int64_t depth, int dtype)
 {
     Shape s{0, 1, 1, 0};
-    if (rows > 16 && cols > 0)
+    if (rows > 0 && cols > 0 && !few_rows(rows, cols, depth))
         shapes_of(&rows, &cols, &depth, 1, dtype, &s);
     return s;
 }
@@ -1154,7 +1164,7 @@ struct GradWork {
     size_t bytes;
 };
 
-// Whether dX and dW can share a launch (those of few rows have a kernel of their own).
+// Whether dX and dW can share a launch (those of few rows mostly have a kernel of their own).
 bool together(int64_t M, int64_t N, int64_t K) { return M > 16 && N > 16 && K > 0; }
 
 void grad_shapes(int64_t M, int64_t N, int64_t K, int dtype, Shape* s)

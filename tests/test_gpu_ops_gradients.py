@@ -65,3 +65,33 @@ def test_a_long_batch_costs_its_work(m, n, k):
     whole = microseconds(lambda: M.linear_grad(dy, x, w))
     half = microseconds(lambda: M.linear_grad(dy[:m // 2], x[:m // 2], w))
     assert whole <= 1.5 * 2 * half, (whole, half)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
+@pytest.mark.parametrize("m,n,k", [(1, 40, 200_000), (16, 100, 70_001), (16, 2048, 8192), (16, 2049, 8192), (3, 2000, 8191),
+                                   (5, 1, 9000), (16, 1, 100_003)])
+def test_few_rows_of_a_deep_product(dtype, m, n, k):
+    g = torch.Generator("cuda").manual_seed(m + n + k)
+    x, w = (ints(g, -2, 2, s, k).to(dtype) for s in (m, n))
+    bias, res = ints(g, -9, 9, n).to(dtype), ints(g, -9, 9, m, n).to(dtype)
+    want = x.double() @ w.double().t().contiguous() + bias.double()
+    y, z = M.linear(x, w, bias=bias, residual=res, act="relu", keep_z=True)
+    assert torch.equal(z, want.to(dtype)) and torch.equal(y, (torch.relu(want) + res.double()).to(dtype))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=ID.get)
+@pytest.mark.parametrize("m,n,k", [(100_000, 1, 128), (100_001, 16, 100), (30_000, 17, 128), (8192, 2, 2500), (8191, 9, 40)])
+def test_gradient_of_few_outputs_over_a_long_batch(dtype, m, n, k):
+    exact(m, n, k, dtype)
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16), ids=ID.get)
+def test_few_rows_cost_no_more_than_many(dtype):
+    """16 outputs over a batch of 100,000 take at most 1.5 times what 17 do, forward and backward."""
+    g = torch.Generator("cuda").manual_seed(2)
+    x, w, dy = (torch.randn(s, generator=g, device="cuda").to(dtype) for s in ((100_000, 128), (17, 128), (100_000, 17)))
+    xt, dyt = x.t().contiguous(), dy.t().contiguous()
+    few, many = (microseconds(lambda: M.linear(dyt[:n], xt)) for n in (16, 17))
+    assert few <= 1.5 * many, (few, many)
+    few, many = (microseconds(lambda: M.linear_grad(dy[:, :n], x, w[:n])) for n in (16, 17))
+    assert few <= 1.5 * many, (few, many)
