@@ -306,8 +306,15 @@ def debug_priority(s: int, stream=None):
 # one, of another dtype than its call's or with strided columns is refused
 # before anything is enqueued, and so is an `out` that shares memory with what
 # the call reads, unless it says that it may.
+#
+# Autograd does not see these calls: they take tensors that require gradients,
+# their results require none, and the ..._grad calls are there to be called.  A
+# tensor changed in place (an `out`, clipped gradients, updated parameters)
+# counts as changed all the same, so that autograd refuses to go backward
+# through a value it had saved of it.
 
 _DTYPES = {torch.float32: FP32, torch.float16: FP16, torch.bfloat16: BF16}
+_changed = torch.autograd.graph.increment_version  # of a tensor or several
 
 
 class _On:
@@ -401,7 +408,8 @@ def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out=None, 
     ld = _matrix(table, "table", on.device)
     idp, stride, count = _ids(ids, on.device)
     rows, k = table.shape
-    if out is None:
+    given = out is not None
+    if not given:
         out = on.empty((count, k), table.dtype)
         ld_out = k
     else:
@@ -409,6 +417,8 @@ def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out=None, 
     on.uses(table, ids, out)
     _check(lib().mfsgd_embed(table.data_ptr(), rows, ld, k, _DTYPES[table.dtype], idp, stride, count, scale,
                              out.data_ptr(), ld_out, on.handle), "mfsgd_embed")
+    if given:
+        _changed(out)
     return out
 
 
@@ -423,7 +433,8 @@ def embed_grad(dout: torch.Tensor, ids: torch.Tensor, rows: int, scale: float = 
     n, k = dout.shape
     if n != count:
         raise ValueError(f"dout has {n} rows for {count} ids")
-    if out is None:
+    given = out is not None
+    if not given:
         if accumulate:
             raise ValueError("accumulate needs an `out` to add to")
         out = on.empty((rows, k), dout.dtype)
@@ -435,6 +446,8 @@ def embed_grad(dout: torch.Tensor, ids: torch.Tensor, rows: int, scale: float = 
     _check(lib().mfsgd_embed_grad(dout.data_ptr(), ld, idp, stride, count, k, _DTYPES[dout.dtype], scale,
                                   out.data_ptr(), rows, ld_out, accumulate, work, nbytes, on.handle),
            "mfsgd_embed_grad")
+    if given:
+        _changed(out)
     return out
 
 
@@ -445,7 +458,8 @@ def rows(side: int, ids: torch.Tensor, k: int, dtype=None, scale: float = 1.0, o
     on = _On(stream)
     idp, stride, count = _ids(ids, on.device)
     dtype = dtype or _storage_dtype()
-    if out is None:
+    given = out is not None
+    if not given:
         out = on.empty((count, k), dtype)
         ld_out = k
     else:
@@ -453,6 +467,8 @@ def rows(side: int, ids: torch.Tensor, k: int, dtype=None, scale: float = 1.0, o
     on.uses(ids, out)
     _check(lib().mfsgd_rows(side, idp, stride, count, k, _DTYPES[dtype], scale, out.data_ptr(), ld_out, on.handle),
            "mfsgd_rows")
+    if given:
+        _changed(out)
     return out
 
 
@@ -493,7 +509,8 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias=None, residual=None, act: str 
         raise ValueError(f"x has {K} columns, w {Kw}")
     bp = None if bias is None else _vector(bias, "bias", N, on.device, dt)
     ldr = 0 if residual is None else _matrix(residual, "residual", on.device, dt, (M, N))
-    if out is None:
+    given = out is not None
+    if not given:
         out = on.empty((M, N), dt)
         ldy = max(N, 1)
     else:
@@ -506,6 +523,8 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias=None, residual=None, act: str 
                               None if residual is None else residual.data_ptr(), ldr, M, N, K, code, ACTS[act],
                               out.data_ptr(), ldy, z.data_ptr() if keep_z else None, max(N, 1), work, nbytes,
                               on.handle), "mfsgd_linear")
+    if given:
+        _changed(out)
     return (out, z) if keep_z else out
 
 
@@ -545,7 +564,8 @@ def scores(users: torch.Tensor, n: int, dtype=None, bias=None, act: str = "none"
     up, stride, count = _ids(users, on.device)
     dtype = dtype or _storage_dtype()
     bp = None if bias is None else _vector(bias, "bias", n, on.device, dtype)
-    if out is None:
+    given = out is not None
+    if not given:
         out = on.empty((count, n), dtype)
         ld = max(n, 1)
     else:
@@ -556,6 +576,8 @@ def scores(users: torch.Tensor, n: int, dtype=None, bias=None, act: str = "none"
     on.uses(users, bias, out)
     _check(lib().mfsgd_scores(up, stride, count, n, _DTYPES[dtype], bp, ACTS[act], out.data_ptr(), ld, work, nbytes,
                               on.handle), "mfsgd_scores")
+    if given:
+        _changed(out)
     return out
 
 
@@ -614,6 +636,7 @@ def clip_grads(grads, max_norm: float, stream=None) -> torch.Tensor:
     work, nbytes, keep = on.workspace(g.workspace_bytes)
     _check(lib().mfsgd_clip_grads(g.entries, len(g), max_norm, norm.data_ptr(), work, nbytes, on.handle),
            "mfsgd_clip_grads")
+    _changed(g.tensors)
     return norm
 
 
@@ -628,6 +651,7 @@ def sgd_step(params, grads, lr: float, lam: float = 0.0, max_norm: float = float
     work, nbytes, keep = on.workspace(g.workspace_bytes)
     _check(lib().mfsgd_sgd_step(p.entries, g.entries, len(g), lr, lam, max_norm, norm.data_ptr(), work, nbytes,
                                 on.handle), "mfsgd_sgd_step")
+    _changed(p.tensors)
     return norm
 
 
