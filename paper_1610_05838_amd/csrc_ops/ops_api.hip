@@ -378,14 +378,23 @@ int norm_impl(const mfsgd_tensor* params, const mfsgd_tensor* grads, int64_t cou
     const size_t need = norm_bytes(count);
     if (int rc = check_work(work, bytes, need))
         return rc;
+    const Span norm{(uintptr_t)norm_dev, (uintptr_t)norm_dev + sizeof(double), true};
+    const Span used{(uintptr_t)work, (uintptr_t)work + need, true};
     std::vector<Span> spans;
     spans.reserve((size_t)count * 2 + 2);
     add_spans(spans, grads, count, apply == 1);
-    if (apply == 2)
-        add_spans(spans, params, count, true);
-    spans.push_back(Span{(uintptr_t)norm_dev, (uintptr_t)norm_dev + sizeof(double), true});
-    spans.push_back(Span{(uintptr_t)work, (uintptr_t)work + need, true});
-    REQUIRE(!overlap(spans), "an array that is written overlaps another one");
+    bool shared = norm.from < used.to && used.from < norm.to;
+    if (apply) {
+        if (apply == 2)
+            add_spans(spans, params, count, true);
+        spans.push_back(norm);
+        spans.push_back(used);
+        shared = overlap(spans);
+    } else { // gradients that are only read may share what they like
+        for (const Span& x : spans)
+            shared |= (x.from < norm.to && norm.from < x.to) || (x.from < used.to && used.from < x.to);
+    }
+    REQUIRE(!shared, "an array that is written overlaps another one");
     std::vector<NormTensor> list((size_t)count);
     for (int64_t i = 0; i < count; ++i)
         list[i] = NormTensor{apply == 2 ? params[i].data : grads[i].data, grads[i].data, grads[i].n, grads[i].dtype};
