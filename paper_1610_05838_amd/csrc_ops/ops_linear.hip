@@ -773,10 +773,10 @@ __global__ __launch_bounds__(256) void k_gemm_few(GemmArgs g, Epilogue e)
 
 // The column sums alone.
 template <typename T>
-__global__ __launch_bounds__(512) void k_dbias(Products p)
+__global__ __launch_bounds__(512) void k_dbias(Products p, uint32_t from)
 {
     __shared__ float lds[8 * 64];
-    add_columns<T, 8>(p, blockIdx.x, lds);
+    add_columns<T, 8>(p, (int64_t)from + blockIdx.x, lds);
 }
 
 // ------------------------------------------------- operands of the gradient
@@ -906,7 +906,7 @@ __global__ __launch_bounds__(kTurnThreads) void k_turn(Turns a)
 }
 
 // ------------------------------------------------------------------- host
-constexpr uint32_t kMostWgs = 1 << 22;
+constexpr uint32_t kMostWgs = 1 << 22; // of a launch: a grid's threads are counted in 32 bits
 constexpr int64_t kCus = 256; // of an MI355X
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to; }
@@ -1265,8 +1265,8 @@ hipError_t grad_typed(const LinearGradLaunch& a, hipStream_t st)
         err = gemm<T>(p.g[0], p.e[0], a.dtype, w.part, st);
     if (a.dw && err == hipSuccess)
         err = gemm<T>(p.g[1], p.e[1], a.dtype, w.part, st);
-    if (sums && err == hipSuccess) {
-        hipLaunchKernelGGL((k_dbias<T>), dim3(sums), dim3(512), 0, st, p);
+    for (uint32_t from = 0; from < sums && err == hipSuccess; from += kMostWgs) {
+        hipLaunchKernelGGL((k_dbias<T>), dim3(std::min(kMostWgs, sums - from)), dim3(512), 0, st, p, from);
         err = hipGetLastError();
     }
     return err;

@@ -95,3 +95,14 @@ def test_few_rows_cost_no_more_than_many(dtype):
     assert few <= 1.5 * many, (few, many)
     few, many = (microseconds(lambda: M.linear_grad(dy[:, :n], x, w[:n])) for n in (16, 17))
     assert few <= 1.5 * many, (few, many)
+
+
+def test_a_bias_of_more_columns_than_one_launch_takes():
+    """2^29 columns: 64 to a workgroup of 512 threads are more threads than a grid counts."""
+    n = (1 << 29) + 100
+    dy = torch.zeros(2, n, dtype=torch.float16, device="cuda")
+    dy[:, -1], dy[1, 0], dy[0, 1 << 28], dy[1, (1 << 29) - 1] = 2.0, 3.0, 5.0, 7.0
+    x, w = torch.zeros(2, 0, dtype=dy.dtype, device="cuda"), torch.zeros(n, 0, dtype=dy.dtype, device="cuda")
+    _, _, db = M.linear_grad(dy, x, w, dx=False, dw=False)
+    at = torch.tensor([0, 1, 1 << 28, (1 << 29) - 1, n - 1], device="cuda")
+    assert db[at].tolist() == [3.0, 0.0, 5.0, 7.0, 4.0] and int(torch.count_nonzero(db)) == 4
