@@ -573,15 +573,16 @@ int mfsgd_linear_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, int64
  *   dZ = dY * act'(Z) elementwise,   dX = dZ W,   dW = dZ^T X,   dbias = column sums of dZ
  * (the residual's gradient is dY).  dx, dw and dbias may be NULL: left out; z may
  * be NULL for MFSGD_ACT_NONE; w may be NULL without dx, x without dw.  The slope
- * of relu at 0 is 0, of an act at NaN is NaN, at an infinity its limit.  dZ is rounded to the dtype before the products (as the
- * matrix instructions take it) and summed unrounded into dbias: with a 16-bit dtype and a sigmoid, silu or
+ * of relu at 0 is 0, of an act at NaN is NaN, at an infinity its limit.  dZ is
+ * rounded to the dtype before the products (as the matrix instructions take it)
+ * and summed unrounded into dbias: with a 16-bit dtype and a sigmoid, silu or
  * gelu, dX and dW then carry two roundings in place of one. */
 int mfsgd_linear_grad(const void* dy, int64_t lddy, const void* z, int64_t ldz, const void* x, int64_t ldx,
                       const void* w, int64_t ldw, int64_t M, int64_t N, int64_t K, int32_t dtype, int32_t act,
                       void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias, void* workspace,
                       int64_t workspace_bytes, void* stream);
-/* EINVAL also for sizes whose matrices are together larger than 2^62 bytes (here and in the call, whichever
- * results it is asked for). */
+/* EINVAL also for sizes whose matrices are together larger than 2^62 bytes (here
+ * and in the call, whichever results it is asked for). */
 int mfsgd_linear_grad_workspace(int64_t M, int64_t N, int64_t K, int32_t dtype, int64_t* bytes);
 
 /* The model's answer: the scores of `count` users against all its items,

@@ -941,9 +941,9 @@ int tile_for(const int64_t* rows, const int64_t* cols, const int64_t* stages, in
         low += up(rows[i], 64) * up(cols[i], 128);
         least = std::min(least, stages[i]);
     }
-    // Large tiles have no slices, so of two products the deeper one's tiles must not be what the launch waits for: up to
-    // 1.25 times the evenly spread stages, which is the rate they gain.  (M, N, K = 24576, 512, 512 bfloat16, where dW is
-    // 4 such tiles of 384 stages: 443 us, 65 with tiles of 128 and slices; 6144, 2048, 2048: 146 and 117.)
+    // Large tiles have no slices, so of two products the deeper one's tiles must not be what the launch waits for:
+    // up to 1.25 times the evenly spread stages, which is the rate they gain.  (M, N, K = 24576, 512, 512 bfloat16,
+    // where dW is 4 such tiles of 384 stages: 443 us, 65 with tiles of 128 and slices; 6144, 2048, 2048: 146, 117.)
     const bool even = n == 1 || (double)most * (double)kCus <= 1.25 * (double)work;
     if (least >= 8 && even && (double)up(big, kCus) <= 0.625 * 0.5 * (double)up(mid, kCus))
         return 256;

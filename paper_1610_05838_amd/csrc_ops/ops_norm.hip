@@ -274,7 +274,8 @@ hipError_t norm_apply(const NormTensor* list, int64_t count, int apply, double m
         if (!a.count)
             break;
         const int64_t wgs = std::min<int64_t>(a.first[a.count], kMostWgs);
-        hipLaunchKernelGGL((once ? k_norm_part<true> : k_norm_part<false>), dim3((unsigned)wgs), dim3(kThreads), 0, st, a, part + parts);
+        hipLaunchKernelGGL((once ? k_norm_part<true> : k_norm_part<false>), dim3((unsigned)wgs), dim3(kThreads), 0, st,
+                           a, part + parts);
         parts += wgs;
     }
     const bool folded = !apply || parts > kFold || parts == 0;
@@ -294,11 +295,11 @@ hipError_t norm_apply(const NormTensor* list, int64_t count, int apply, double m
             break;
         const int64_t wgs = std::min<int64_t>(a.first[a.count], kMostWgs);
         if (apply == 2)
-            hipLaunchKernelGGL((once ? k_norm_apply<true, true> : k_norm_apply<true, false>), dim3((unsigned)wgs), dim3(kThreads), 0, st, a, part, parts,
-                               max_norm, lr, lam, norm);
+            hipLaunchKernelGGL((once ? k_norm_apply<true, true> : k_norm_apply<true, false>), dim3((unsigned)wgs),
+                               dim3(kThreads), 0, st, a, part, parts, max_norm, lr, lam, norm);
         else
-            hipLaunchKernelGGL((once ? k_norm_apply<false, true> : k_norm_apply<false, false>), dim3((unsigned)wgs), dim3(kThreads), 0, st, a, part, parts,
-                               max_norm, lr, lam, norm);
+            hipLaunchKernelGGL((once ? k_norm_apply<false, true> : k_norm_apply<false, false>), dim3((unsigned)wgs),
+                               dim3(kThreads), 0, st, a, part, parts, max_norm, lr, lam, norm);
         norm = nullptr; // written by the first
     }
     return hipGetLastError();

@@ -27,12 +27,12 @@ constexpr int64_t kMostWgs = 1 << 22; // of a launch; workgroups then take sever
 // thread has kAhead rows' loads in flight: the ids first, then the rows.  40,960
 // rows of 1,000 bytes (68 MB with padding and repeated rows): 10.4 us; 50 rows of
 // 256 bytes: 2.2 us, a launch and two trips to memory.
-constexpr int kAhead = 4;
-
 //
 // ONCE: past the caches, where `out` is larger than the Infinity Cache and its
 // rows are whole cache lines (1.4 M rows of 512 bytes: 202 us, 4.2 TB/s, against
 // 225; 41 MB that stay in the caches: 11.7 us against 10.4).
+constexpr int kAhead = 4;
+
 template <typename T, int V, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_rows_get(const T* __restrict__ table, int64_t rows, int64_t ld, int k,
                                                        const int32_t* __restrict__ ids, int64_t ids_stride,

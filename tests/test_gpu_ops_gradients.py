@@ -106,3 +106,42 @@ def test_a_bias_of_more_columns_than_one_launch_takes():
     _, _, db = M.linear_grad(dy, x, w, dx=False, dw=False)
     at = torch.tensor([0, 1, 1 << 28, (1 << 29) - 1, n - 1], device="cuda")
     assert db[at].tolist() == [3.0, 0.0, 5.0, 7.0, 4.0] and int(torch.count_nonzero(db)) == 4
+
+
+def test_more_rows_than_one_launch_takes():
+    """2^29 rows: more tiles than a launch has workgroups, and rows of the exchanged matrices that pass 32 bits."""
+    m = (1 << 29) + 100
+    x = torch.zeros(m, 2, dtype=torch.float16, device="cuda")
+    at = torch.tensor([0, 1 << 28, (1 << 29) - 1, 1 << 29, m - 1], device="cuda")
+    x[at] = torch.tensor([[1, 2], [3, 4], [5, 6], [7, 8], [9, 10]], dtype=torch.float16, device="cuda")
+    w = torch.tensor([[2.0, -1.0]], dtype=torch.float16, device="cuda")
+    y = M.linear(x, w)
+    assert y[at, 0].tolist() == [0.0, 2.0, 4.0, 6.0, 8.0] and int(torch.count_nonzero(y)) == 4
+    y[0] = 1.0
+    dx, dw, db = M.linear_grad(y, x, w)
+    assert dx[at].tolist() == [[2.0 * d, -d] for d in (1.0, 2.0, 4.0, 6.0, 8.0)]
+    assert int(torch.count_nonzero(dx[:, 0])) == 5
+    assert dw.tolist() == [[1.0 + 6 + 20 + 42 + 72, 2.0 + 8 + 24 + 48 + 80]] and db.tolist() == [21.0]
+
+
+def test_captured_with_slices():
+    """Forms that join slices, in a graph: every replay sees the inputs as they are then."""
+    g = torch.Generator("cuda").manual_seed(3)
+    data = [tuple(torch.randn(s, generator=g, device="cuda").bfloat16() for s in ((m, k), (n, k), (m, n)))
+            for m, n, k in ((3, 200, 9000), (20_000, 2, 130), (24_576, 256, 256))]
+
+    def run():
+        return [(M.linear(x, w, residual=r, act="gelu"), *M.linear_grad(r, x, w, z=r, act="gelu")) for x, w, r in data]
+
+    run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = run()
+    for _ in range(4):
+        for t in data:
+            for a in t:
+                a.copy_(torch.randn(a.shape, generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, run()):
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
