@@ -530,7 +530,8 @@ int mfsgd_embed(const void* table, int64_t rows, int64_t ld, int32_t k, int32_t 
 int mfsgd_embed_grad(const void* dout, int64_t ld_dout, const int32_t* ids, int64_t ids_stride, int64_t count,
                      int32_t k, int32_t dtype, float scale, void* dtable, int64_t rows, int64_t ld,
                      int32_t accumulate, void* workspace, int64_t workspace_bytes, void* stream);
-int mfsgd_embed_grad_workspace(int64_t count, int32_t k, int64_t* bytes);
+int mfsgd_embed_grad_workspace(int64_t count, int32_t k, int64_t* bytes); /* enough for any table */
+int mfsgd_embed_grad_workspace_rows(int64_t count, int32_t k, int64_t rows, int64_t* bytes); /* of `rows` rows */
 
 /* The two on the model's own factors (after mfsgd_init; the current device must
  * be the one it ran on): `side` is MFSGD_P (users, m rows) or MFSGD_Q (items, n

@@ -182,7 +182,7 @@ int embed_grad_impl(RowsGradLaunch a, void* work, int64_t bytes, void* stream)
         return rc;
     REQUIRE(matrix_ok(a.dout, a.count, a.k, a.ld_dout, a.dtype), "dout is NULL or misaligned, or ld_dout is below k");
     REQUIRE(matrix_ok(a.dtable, a.rows, a.k, a.ld, a.dtype), "dtable is NULL or misaligned, or ld is below k");
-    const size_t need = rows_grad_bytes(a.count, a.k);
+    const size_t need = rows_grad_bytes(a.count, a.k, a.rows);
     if (int rc = check_work(work, bytes, need))
         return rc;
     if (int rc = check_apart({matrix(a.dout, a.count, a.k, a.ld_dout, a.dtype),
@@ -426,11 +426,17 @@ int mfsgd_embed_grad(const void* dout, int64_t ld_dout, const int32_t* ids, int6
 
 int mfsgd_embed_grad_workspace(int64_t count, int32_t k, int64_t* bytes)
 {
+    return mfsgd_embed_grad_workspace_rows(count, k, 1, bytes);
+}
+
+int mfsgd_embed_grad_workspace_rows(int64_t count, int32_t k, int64_t rows, int64_t* bytes)
+{
     return guarded([&]() -> int {
         REQUIRE(bytes, "NULL bytes");
         REQUIRE(count >= 0 && count <= INT32_MAX, "count must be in [0, 2^31-1]");
         REQUIRE(k >= 1 && k <= kMostColumns, "k must be in [1, 2^22]");
-        *bytes = (int64_t)rows_grad_bytes(count, k);
+        REQUIRE(rows >= 1 && rows <= INT32_MAX, "rows must be in [1, 2^31-1]");
+        *bytes = (int64_t)rows_grad_bytes(count, k, rows);
         return MFSGD_OK;
     });
 }

@@ -56,7 +56,7 @@ struct RowsGradLaunch {
     int accumulate;
     void* work;
 };
-size_t rows_grad_bytes(int64_t count, int k);
+size_t rows_grad_bytes(int64_t count, int k, int64_t rows); // most for rows = 1
 hipError_t rows_grad(const RowsGradLaunch& a, hipStream_t st);
 
 // ---- products (ops_linear.hip) ----

@@ -192,7 +192,12 @@ __global__ __launch_bounds__(kThreads) void k_rows_zero(T* __restrict__ out, int
 // the comparisons, the most frequent row's sum.  4,001 Zipf tokens of 64 binary32:
 // 13 us, sorting them 30; 8,192: 26 and 31 (512 bfloat16: 36 and 36); beyond that
 // the comparisons, square in the number of tokens, outweigh the sort's launches.
+// A row with much of the tokens is one workgroup's chain, 11 to 30 us per 1,000 of
+// them, so a table whose rows have more than kScanAlone on average is sorted for
+// from kScanSurely tokens on (8,192 of 512 binary32 for 10 rows: 22 us for 97; 4,000
+// of 128 for 3 rows: 21 for 59, for 30 rows: 20 for 27).
 constexpr int kScanMost = 8192;
+constexpr int kScanSurely = 2048;
 constexpr int kScanAlone = 64;
 constexpr int kScanBlock = 256; // ids compared at a time: four a lane
 
@@ -843,6 +848,11 @@ hipError_t zero_typed(const RowsGradLaunch& a, hipStream_t st)
     return v == 4 ? zero_launch<T, 4>(a, st) : v == 2 ? zero_launch<T, 2>(a, st) : zero_launch<T, 1>(a, st);
 }
 
+bool scanned(int64_t count, int64_t rows)
+{
+    return count <= kScanSurely || (count <= kScanMost && count <= rows * kScanAlone);
+}
+
 // Tokens of a tile: 64 (a lane each), or fewer (at least 16) where that leaves
 // the chip without 4096 wavefronts.  Half the tiles that it holds at once are as
 // fast as all of them, and long rows then have half as many parts to join
@@ -911,7 +921,7 @@ template <typename T, int E>
 hipError_t grad_launch(const RowsGradLaunch& a, hipStream_t st)
 {
     const unsigned ys = (unsigned)((a.k + 64 * E - 1) / (64 * E));
-    if (a.count <= kScanMost) {
+    if (scanned(a.count, a.rows)) {
         if (!a.accumulate && a.rows > 0) {
             const hipError_t e = zero_typed<T>(a, st);
             if (e != hipSuccess)
@@ -972,7 +982,10 @@ hipError_t rows_get(const RowsLaunch& a, hipStream_t st)
     return get_typed<float>(a, st);
 }
 
-size_t rows_grad_bytes(int64_t count, int k) { return count <= kScanMost ? 0 : grad_work(count, k, nullptr).bytes; }
+size_t rows_grad_bytes(int64_t count, int k, int64_t rows)
+{
+    return scanned(count, rows) ? 0 : grad_work(count, k, nullptr).bytes;
+}
 
 hipError_t rows_grad(const RowsGradLaunch& a, hipStream_t st)
 {

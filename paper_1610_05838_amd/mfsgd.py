@@ -79,6 +79,7 @@ def lib():
             "mfsgd_embed": ([vp, i64, i64, i32, i32, vp, i64, i64, f32, vp, i64, vp], C.c_int),
             "mfsgd_embed_grad": ([vp, i64, vp, i64, i64, i32, i32, f32, vp, i64, i64, i32, vp, i64, vp], C.c_int),
             "mfsgd_embed_grad_workspace": ([i64, i32, C.POINTER(i64)], C.c_int),
+            "mfsgd_embed_grad_workspace_rows": ([i64, i32, i64, C.POINTER(i64)], C.c_int),
             "mfsgd_rows": ([i32, vp, i64, i64, i32, i32, f32, vp, i64, vp], C.c_int),
             "mfsgd_add_rows": ([i32, vp, i64, vp, i64, i64, i32, i32, f32, vp, i64, vp], C.c_int),
             "mfsgd_linear": ([vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp],
@@ -397,10 +398,6 @@ def _bytes(fn, *sizes):
     return n.value
 
 
-def _grad_workspace(on, count, k):
-    return on.workspace(_bytes("mfsgd_embed_grad_workspace", count, k))
-
-
 def embed(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, out=None, stream=None) -> torch.Tensor:
     """Rows of `table` by id, times `scale`; zeros where an id is outside the
     table (padding).  `ids` may be a column of a sample tensor."""
@@ -441,7 +438,7 @@ def embed_grad(dout: torch.Tensor, ids: torch.Tensor, rows: int, scale: float = 
         ld_out = k
     else:
         ld_out = _matrix(out, "out", on.device, dout.dtype, (rows, k))
-    work, nbytes, keep = _grad_workspace(on, count, k)
+    work, nbytes, keep = on.workspace(_bytes("mfsgd_embed_grad_workspace_rows", count, k, rows))
     on.uses(dout, ids, out)
     _check(lib().mfsgd_embed_grad(dout.data_ptr(), ld, idp, stride, count, k, _DTYPES[dout.dtype], scale,
                                   out.data_ptr(), rows, ld_out, accumulate, work, nbytes, on.handle),
@@ -482,7 +479,7 @@ def add_rows(side: int, dout: torch.Tensor, ids: torch.Tensor, scale: float, str
     n, k = dout.shape
     if n != count:
         raise ValueError(f"dout has {n} rows for {count} ids")
-    work, nbytes, keep = _grad_workspace(on, count, k)
+    work, nbytes, keep = on.workspace(_bytes("mfsgd_embed_grad_workspace", count, k))
     on.uses(dout, ids)
     _check(lib().mfsgd_add_rows(side, dout.data_ptr(), ld, idp, stride, count, k, _DTYPES[dout.dtype], scale, work,
                                 nbytes, on.handle), "mfsgd_add_rows")

@@ -52,3 +52,18 @@ def test_a_bias_gradient_of_a_refused_size_is_refused(lib):
     """dbias alone takes no matrix of K columns, but the workspace is laid out for one."""
     args = (A, 1, None, 0, None, 0, None, 0, INT32_MAX, 1, INT32_MAX, 0, 0, None, 0, None, 0, B, D, (1 << 63) - 1, None)
     refused(lib, "mfsgd_linear_grad", args, b"workspace")
+
+
+def test_embed_grad_workspace_of_a_table(lib):
+    """Never more than the one that is enough for any table, and the call asks for no more."""
+    any_table, n = C.c_int64(-1), C.c_int64(-1)
+    for count in (0, 1, 2048, 2049, 8192, 8193, 300_000):
+        assert lib.mfsgd_embed_grad_workspace(count, 40, C.byref(any_table)) == 0
+        for rows in (1, 3, 100, 1_000_000, INT32_MAX):
+            assert lib.mfsgd_embed_grad_workspace_rows(count, 40, rows, C.byref(n)) == 0
+            assert 0 <= n.value <= any_table.value
+    for count, k, rows in ((-1, 8, 5), (INT32_MAX + 1, 8, 5), (5, 0, 5), (5, 8, 0), (5, 8, -1), (5, 8, INT32_MAX + 1)):
+        refused(lib, "mfsgd_embed_grad_workspace_rows", (count, k, rows, C.byref(n)), b"must be")
+    refused(lib, "mfsgd_embed_grad_workspace_rows", (5, 8, 5, None), b"NULL")
+    # 5,000 tokens of 3 rows need one
+    refused(lib, "mfsgd_embed_grad", (A, 8, B, 1, 5000, 8, 0, 1.0, D, 3, 8, 0, None, 0, None), b"workspace")
