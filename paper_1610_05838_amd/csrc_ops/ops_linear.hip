@@ -24,10 +24,10 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 //
 // In binary32.  16-bit results take the hardware's exponential and reciprocal (1
 // ulp) and for the normal distribution's tail the fit below; binary32 results the
-// library functions.  None subtracts two numbers near each other, so that the
-// tails too are right relative to their own size: to the error of exp(-z^2 / 2)
-// with a rounded argument, z^2 2^-22, and in 16 bits to 3e-5 (a 16th of half a step
-// of binary16).
+// library functions.  No small result is the difference of two large numbers, so
+// that the tails too are right relative to their own size: to the error of
+// exp(-z^2 / 2) with a rounded argument, z^2 2^-22, and in 16 bits to 3e-5 (a 16th of
+// half a step of binary16).
 enum { kNone = 0, kRelu = 1, kSigmoid = 2, kSilu = 3, kGelu = 4 };
 
 template <bool EXACT>
